@@ -265,6 +265,69 @@ int mapl_codebook_pack(int32_t L, int32_t K, int64_t r, const float* C, const in
 int mapl_codebook_unpack(int32_t L, int32_t K, int64_t r, const float* buf, const int32_t* rows,
                          int32_t n, float* C, void* stream);
 
+/* Activations kept in 8 bits between forward and backward (what a stage holds
+ * of every micro-batch in flight; the sender's backward, Sec. 3.2, needs X).
+ * Blocks of 32 consecutive tokens of one channel share a power-of-two scale:
+ *   a = max |X[t,c]| over the block, e = max(floor(log2 a), -120)
+ *   q[t] = X[t,c] 2^(6-e) rounded to the nearest integer (ties to even),
+ *          at most 127 in magnitude; it stands for q 2^(e-6)
+ * so a value is off by at most 2^(e-7), the largest ones of a block (within a
+ * 64th of 2^(e+1)) by at most 2^(e-6); X that is such a value already comes
+ * back exactly.  A block that holds a NaN or an infinity comes back as NaNs.
+ *   q [ceil(T/32), d, 32] int8 (token t of channel c at [t/32, c, t%32];
+ *     tokens past T are 0), e [ceil(T/32), d] uint8: e + 127, or 255 for a
+ *     block that stands for NaNs
+ * 1.03 bytes per value.  x_dtype is MAPL_BF16 or MAPL_F32; unpack gives the
+ * same values in either (they are exact in bf16).  0 <= T < 2^31, d as in
+ * mapl_codec_desc.  No workspace. */
+int mapl_ckpt_pack(int64_t T, int64_t d, int32_t x_dtype, const void* X, int8_t* q, uint8_t* e, void* stream);
+int mapl_ckpt_unpack(int64_t T, int64_t d, int32_t x_dtype, const int8_t* q, const uint8_t* e, void* X, void* stream);
+
+/* mapl_encode_bwd with X read from its 8-bit checkpoint (mapl_ckpt_pack of the
+ * descriptor's T and d): the same outputs as mapl_encode_bwd on what
+ * mapl_ckpt_unpack gives.  Workspace: mapl_ckpt_encode_bwd_workspace_bytes. */
+int mapl_ckpt_encode_bwd(const mapl_codec_desc* desc, const void* dZ, const int8_t* q, const uint8_t* e,
+                         const int32_t* ids, const float* U, const void* A_s, const void* B_s, void* dX, float* dU,
+                         int accumulate_dU, void* ws, size_t ws_bytes, void* stream);
+size_t mapl_ckpt_encode_bwd_workspace_bytes(const mapl_codec_desc* desc);
+
+/* The last stage's loss: softmax cross entropy over the vocabulary of the
+ * logits l[t,v] = sum_c H[t,c] W[v,c], which are never kept.
+ *   T tokens, 0 <= T <= 2^22; d, multiple of 64, 64 <= d <= 16384;
+ *   V vocabulary entries, 1 <= V <= 2^22 (any, no multiple needed)
+ *   x_dtype   MAPL_BF16 or MAPL_F32: H [T,d], W [V,d], dH [T,d]
+ *   dw_dtype  of dW [V,d]: MAPL_F32, or MAPL_BF16 with bf16 inputs
+ *   targets [T] int32: 0 <= y < V, or negative: the token is masked, it has
+ *     loss 0, a zero row in dH and no part in dW, whatever its row of H holds.
+ *     A target at or past V is the caller's error (MAPL_DEBUG=1 checks them).
+ * mapl_xent_fwd:
+ *   lse[t] = log sum_v exp(l[t,v]) (masked tokens too),
+ *   loss[t] = lse[t] - l[t, y_t]                          [T] fp32
+ * mapl_xent_bwd, from the forward's lse:
+ *   dl[t,v] = weight[t] (exp(l[t,v] - lse[t]) - (v == y_t))
+ *   dH[t] = scale sum_v dl[t,v] W[v],   dW[v] (+)= scale sum_t dl[t,v] H[t]
+ *   weight [T] fp32, or NULL for ones (a weight of 0 masks the token); scale is
+ *   the factor all tokens share (1 / tokens for a mean).  accumulate_dW = 0
+ *   overwrites dW, 1 adds to it (micro-batches of a step).  dH or dW may be
+ *   NULL (a frozen head, or a first-layer probe): its product is left out.
+ * bf16: logits, statistics and sums in fp32; dl is rounded to bf16 (before
+ * scale, so that the 1 of a target stays exact) for its two products, and dW
+ * in bf16 is rounded once per call.  Results are bitwise reproducible.
+ * Workspace: mapl_xent_workspace_bytes(desc, MAPL_XENT_FWD or _BWD); the
+ * backward's holds dl of a piece of the vocabulary at a time (512 MiB, or 512
+ * bytes a token where that is more). */
+enum mapl_xent_call { MAPL_XENT_FWD = 0, MAPL_XENT_BWD = 1 };
+typedef struct mapl_xent_desc {
+  int64_t T, d, V;
+  int32_t x_dtype, dw_dtype;
+} mapl_xent_desc;
+int mapl_xent_fwd(const mapl_xent_desc* desc, const void* H, const void* W, const int32_t* targets, float* loss,
+                  float* lse, void* ws, size_t ws_bytes, void* stream);
+int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const void* W, const int32_t* targets, const float* lse,
+                  const float* weight, float scale, void* dH, void* dW, int accumulate_dW, void* ws, size_t ws_bytes,
+                  void* stream);
+size_t mapl_xent_workspace_bytes(const mapl_xent_desc* desc, int call);
+
 /* mapl_encode without a workspace, for callers that cannot allocate device
  * memory (code under HIP graph capture, tight serving loops, harnesses that
  * forbid hipMalloc).  Same arguments, results and errors as mapl_encode;

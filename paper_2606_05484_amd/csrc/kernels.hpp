@@ -337,6 +337,61 @@ struct AnchorSegArgs {
 int anchor_sub_chunks(int n);
 hipError_t launch_anchor_segsum(const AnchorSegArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------- 8-bit checkpoints
+// q [ceil(T/32)][d][32] int8 and the exponents [ceil(T/32)][d] of X [T][d]
+// (fp32 or bf16), and back (see k_ckpt.hip for the format).
+hipError_t launch_ckpt_pack(const void* X, int f32, int64_t T, int d, void* q, uint8_t* e, hipStream_t s);
+hipError_t launch_ckpt_unpack(const void* q, const uint8_t* e, int64_t T, int d, void* X, int f32, hipStream_t s);
+
+// ---------------------------------------------------------------- vocabulary cross entropy
+// Products of bf16 operands, C(m, n) = sum_k P(m, k) Q(n, k): M x N, K split
+// into runs of kper (a multiple of 64; 0: one run).  Leading dimensions are
+// multiples of 8 and at most 2^21.
+struct XentGemm {
+  const bf16_t* P; int64_t ldp;
+  const bf16_t* Q; int64_t ldq;
+  int M, N; int64_t K, kper;
+};
+struct XentTok {
+  const int32_t* y;     // [T] targets, negative: masked
+  const float* weight;  // [T] or null (ones)
+};
+// M = vocabulary, N = tokens, K = d % 64 == 0, both operands [row][k].
+// part [xent_partials(V, T)][T][2] (maximum, sum of exp), tgt [T] the targets' logits.
+int xent_partials(int64_t V, int64_t T);
+hipError_t launch_xent_lse(const XentGemm& q, const XentTok& a, float* part, float* tgt, hipStream_t s);
+hipError_t launch_xent_join(const float* part, int np, int T, const XentTok& a, const float* tgt, float* loss, float* lse,
+                            hipStream_t s);
+// tok [T][4]: lse log2 e, weight (0: masked), target; Hm (may be null): H with
+// the masked rows zero.
+hipError_t launch_xent_prep(const void* H, int esize, int T, int d, const XentTok& a, const float* lse, float* tok, void* Hm,
+                            hipStream_t s);
+// dl [T][ld] of the vocabulary piece that starts at v0 (q.P its rows, q.M of
+// them); columns q.M .. ld are zeros, ld a multiple of 64.
+hipError_t launch_xent_dl(const XentGemm& q, const float* tok, int v0, bf16_t* dl, int64_t ld, hipStream_t s);
+// out[n][m] (+)= scale C(m, n), M % 64 == 0; P is [k][m] (what lies past its
+// K-th row reads as zero), Q [n][k] (K padded to 64 with readable columns) or
+// with q_along_rows [k][n].  splits > 1: fp32 out + split * split_stride.  tok
+// given: rows of tokens with weight 0 are zeros.
+struct XentOut {
+  void* out; int64_t ld; int f32, add;
+  float scale;
+  const float4* tok;
+  int64_t split_stride;
+};
+bool xent_big_tiles(int64_t M, int64_t N, int64_t splits);
+hipError_t launch_xent_out(const XentGemm& q, int q_along_rows, const XentOut& o, hipStream_t s);
+hipError_t launch_xent_sum(const float* part, int splits, int T, int d, const float* tok, float scale, bf16_t* dH,
+                           hipStream_t s);
+// fp32: n logits per token in rows of ld; dl over them in place (times scale, zeros up to ld).
+hipError_t launch_xent_lse_f32(const float* l, int64_t ld, int T, int n, int v0, const XentTok& a, float* part, float* tgt,
+                               hipStream_t s);
+hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, const float* lse, const XentTok& a, float scale,
+                              hipStream_t s);
+hipError_t launch_xent_zero_rows(float* X, int T, int d, const XentTok& a, hipStream_t s);
+// flag[0] = 1 if any y[t] >= V.
+hipError_t launch_xent_check(const int32_t* y, int T, int64_t V, int* flag, hipStream_t s);
+
 // ---------------------------------------------------------------- debug
 // flag[0] = 1 if any ids[t] is outside [0, V).
 hipError_t launch_check_ids(const int32_t* ids, int T, int64_t V, int* flag, hipStream_t s);

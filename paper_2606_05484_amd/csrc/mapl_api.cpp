@@ -846,9 +846,23 @@ extern "C" int mapl_grad_dequantize(int64_t T, int64_t r, int32_t Lg, int32_t Kg
 }
 
 // ----------------------------------------------------------------- encode_bwd
-extern "C" int mapl_encode_bwd(const mapl_codec_desc* desc, const void* dZ, const void* X, const int32_t* ids,
-                               const float* U, const void* A_s, const void* B_s, void* dX, float* dU,
-                               int accumulate_dU, void* ws, size_t ws_bytes, void* stream) {
+namespace {
+size_t ckpt_q_bytes(int64_t T, int64_t d) { return (size_t)((T + 31) / 32) * 32 * d; }
+size_t ckpt_e_bytes(int64_t T, int64_t d) { return (size_t)((T + 31) / 32) * d; }
+
+// The workspace of encode_bwd from a checkpoint: encode_bwd's, then X.
+size_t ckpt_x_offset(const mapl_codec_desc& D) { return layout(D, MAPL_CALL_ENCODE_BWD).total; }
+size_t ckpt_ws_bytes(const mapl_codec_desc& D) {
+  Carve c;
+  c.take(ckpt_x_offset(D));
+  c.take((size_t)D.T * D.d * esize(D.x_dtype));
+  return c.off;
+}
+
+// mapl_encode_bwd on X, or (ck) mapl_ckpt_encode_bwd on X's checkpoint (q, e).
+int encode_bwd(const mapl_codec_desc* desc, const void* dZ, const void* X, bool ck, const int8_t* q, const uint8_t* e,
+               const int32_t* ids, const float* U, const void* A_s, const void* B_s, void* dX, float* dU,
+               int accumulate_dU, void* ws, size_t ws_bytes, void* stream) {
   g_err.clear();
   int st = check_desc(desc);
   if (st) return st;
@@ -857,14 +871,15 @@ extern "C" int mapl_encode_bwd(const mapl_codec_desc* desc, const void* dZ, cons
   const size_t xe = esize(D.x_dtype);
   const bool amb = D.anchor_space == MAPL_ANCHOR_AMBIENT;
   const bool need_anchor = amb && k > 0;
-  st = check_ptrs({{dZ, (size_t)T * r * xe, "dZ"}, {X, (size_t)T * d * xe, "X"},
+  const size_t xb = ck ? 0 : (size_t)T * d * xe, qb = ck ? ckpt_q_bytes(T, d) : 0, eb = ck ? ckpt_e_bytes(T, d) : 0;
+  st = check_ptrs({{dZ, (size_t)T * r * xe, "dZ"}, {X, xb, "X"}, {q, qb, "q"}, {e, eb, "e"},
                    {ids, need_anchor ? (size_t)T * 4 : 0, "ids"}, {U, (size_t)d * r * 4, "U"},
                    {A_s, need_anchor ? (size_t)D.V * k * xe : 0, "A_s"},
                    {B_s, need_anchor ? (size_t)k * d * xe : 0, "B_s"}, {dX, (size_t)T * d * xe, "dX"},
                    {dU, (size_t)d * r * 4, "dU"}},
                   {{dX, (size_t)T * d * xe, "dX"}, {dU, (size_t)d * r * 4, "dU"}},
-                  {{dZ, (size_t)T * r * xe, "dZ"}, {X, (size_t)T * d * xe, "X"}, {ids, (size_t)T * 4, "ids"},
-                   {U, (size_t)d * r * 4, "U"}, {A_s, (size_t)D.V * k * xe, "A_s"},
+                  {{dZ, (size_t)T * r * xe, "dZ"}, {X, xb, "X"}, {q, qb, "q"}, {e, eb, "e"},
+                   {ids, (size_t)T * 4, "ids"}, {U, (size_t)d * r * 4, "U"}, {A_s, (size_t)D.V * k * xe, "A_s"},
                    {B_s, (size_t)k * b_cols(D) * xe, "B_s"}, {ws, ws_bytes, "workspace"}});
   if (st) return st;
   if (dX && dU) {
@@ -872,12 +887,17 @@ extern "C" int mapl_encode_bwd(const mapl_codec_desc* desc, const void* dZ, cons
     if (a0 < b1 && b0 < a1) return fail(MAPL_E_ALIAS, "output dX overlaps output dU");
   }
   const Layout Lo = layout(D, MAPL_CALL_ENCODE_BWD);
-  if ((st = check_ws(ws, ws_bytes, Lo.total))) return st;
+  if ((st = check_ws(ws, ws_bytes, ck ? ckpt_ws_bytes(D) : Lo.total))) return st;
   hipStream_t s = (hipStream_t)stream;
   if (need_anchor && (st = run_id_check(ids, T, D.V, ws, Lo, s))) return st;
   if (T == 0) {
     if (!accumulate_dU) LAUNCH("enc_bwd:zero_bytes", launch_zero_bytes(dU, d * r * 4, s));
     return MAPL_OK;
+  }
+  if (ck) {
+    void* Xq = at<char>(ws, ckpt_x_offset(D));
+    LAUNCH("enc_bwd:unpack", launch_ckpt_unpack(q, e, T, (int)d, Xq, D.x_dtype == MAPL_F32, s));
+    X = Xq;
   }
 
   if (D.x_dtype == MAPL_BF16) {
@@ -961,6 +981,13 @@ extern "C" int mapl_encode_bwd(const mapl_codec_desc* desc, const void* dZ, cons
     LAUNCH("enc_bwd:gemm_f32", launch_gemm_f32(g, s));
   }
   return MAPL_OK;
+}
+}  // namespace
+
+extern "C" int mapl_encode_bwd(const mapl_codec_desc* desc, const void* dZ, const void* X, const int32_t* ids,
+                               const float* U, const void* A_s, const void* B_s, void* dX, float* dU,
+                               int accumulate_dU, void* ws, size_t ws_bytes, void* stream) {
+  return encode_bwd(desc, dZ, X, false, nullptr, nullptr, ids, U, A_s, B_s, dX, dU, accumulate_dU, ws, ws_bytes, stream);
 }
 
 // ---------------------------------------------------------------- stiefel
@@ -1413,6 +1440,284 @@ extern "C" int mapl_encode_noalloc(const mapl_codec_desc* desc, const void* X, c
   void* ws = nullptr;
   if ((st = scratch_for_current_device(&ws))) return st;
   return mapl_encode(desc, X, ids, U, A_s, B_s, C, payload, ws, (size_t)MAPL_NOALLOC_SCRATCH_BYTES, stream);
+}
+
+// ------------------------------------------------------------ 8-bit checkpoints
+namespace {
+int check_ckpt(int64_t T, int64_t d, int x_dtype) {
+  if (x_dtype != MAPL_BF16 && x_dtype != MAPL_F32)
+    return fail(MAPL_E_DTYPE, "x_dtype must be MAPL_BF16 or MAPL_F32 (got %d)", x_dtype);
+  if (T < 0 || T >= ((int64_t)1 << 31)) return fail(MAPL_E_SHAPE, "T=%lld out of range", (long long)T);
+  if (d < 64 || d > 16384 || d % 64)
+    return fail(MAPL_E_SHAPE, "d=%lld: need 64 <= d <= 16384, d %% 64 == 0", (long long)d);
+  return MAPL_OK;
+}
+}  // namespace
+
+extern "C" int mapl_ckpt_pack(int64_t T, int64_t d, int32_t x_dtype, const void* X, int8_t* q, uint8_t* e, void* stream) {
+  g_err.clear();
+  int st = check_ckpt(T, d, x_dtype);
+  if (st) return st;
+  const size_t xb = (size_t)T * d * esize(x_dtype), qb = ckpt_q_bytes(T, d), eb = ckpt_e_bytes(T, d);
+  st = check_ptrs({{X, xb, "X"}, {q, qb, "q"}, {e, eb, "e"}}, {{q, qb, "q"}, {e, eb, "e"}}, {{X, xb, "X"}});
+  if (!st) st = check_ptrs({}, {{q, qb, "q"}}, {{e, eb, "e"}});
+  if (st) return st;
+  if (T == 0) return MAPL_OK;
+  hipStream_t s = (hipStream_t)stream;
+  LAUNCH("ckpt:pack", launch_ckpt_pack(X, x_dtype == MAPL_F32, T, (int)d, q, e, s));
+  return MAPL_OK;
+}
+
+extern "C" int mapl_ckpt_unpack(int64_t T, int64_t d, int32_t x_dtype, const int8_t* q, const uint8_t* e, void* X,
+                                void* stream) {
+  g_err.clear();
+  int st = check_ckpt(T, d, x_dtype);
+  if (st) return st;
+  const size_t xb = (size_t)T * d * esize(x_dtype), qb = ckpt_q_bytes(T, d), eb = ckpt_e_bytes(T, d);
+  st = check_ptrs({{q, qb, "q"}, {e, eb, "e"}, {X, xb, "X"}}, {{X, xb, "X"}}, {{q, qb, "q"}, {e, eb, "e"}});
+  if (st) return st;
+  if (T == 0) return MAPL_OK;
+  hipStream_t s = (hipStream_t)stream;
+  LAUNCH("ckpt:unpack", launch_ckpt_unpack(q, e, T, (int)d, X, x_dtype == MAPL_F32, s));
+  return MAPL_OK;
+}
+
+extern "C" size_t mapl_ckpt_encode_bwd_workspace_bytes(const mapl_codec_desc* desc) {
+  g_err.clear();
+  if (check_desc(desc) != MAPL_OK) return 0;
+  return ckpt_ws_bytes(*desc);
+}
+
+extern "C" int mapl_ckpt_encode_bwd(const mapl_codec_desc* desc, const void* dZ, const int8_t* q, const uint8_t* e,
+                                    const int32_t* ids, const float* U, const void* A_s, const void* B_s, void* dX,
+                                    float* dU, int accumulate_dU, void* ws, size_t ws_bytes, void* stream) {
+  return encode_bwd(desc, dZ, nullptr, true, q, e, ids, U, A_s, B_s, dX, dU, accumulate_dU, ws, ws_bytes, stream);
+}
+
+// ---------------------------------------------------- vocabulary cross entropy
+namespace {
+// dl of one vocabulary piece (bf16), or its fp32 logits, in the workspace
+constexpr int64_t kXentPieceBytes = (int64_t)512 << 20;
+constexpr int64_t kXentMaxPiece = (int64_t)1 << 21;  // columns (32-bit offsets inside a tile's panel)
+
+struct XentLayout {
+  size_t total = 0, flag = 0, part = 0, tgt = 0, tok = 0, hm = 0, dl = 0, acc = 0;
+  int64_t piece = 0, ld = 0, kper = 0;  // vocabulary entries per piece, a row of dl, dH's run of K
+  int pieces = 1, splits = 1;
+};
+
+XentLayout xent_layout(const mapl_xent_desc& D, int call) {
+  XentLayout L;
+  Carve c;
+  const bool bf = D.x_dtype == MAPL_BF16;
+  const int64_t es = bf ? 2 : 4, T = D.T > 0 ? D.T : 1;
+  L.flag = c.take(256);
+  int64_t piece = kXentPieceBytes / (es * T) / 256 * 256;
+  if (piece < 256) piece = 256;
+  if (piece > kXentMaxPiece) piece = kXentMaxPiece;
+  L.pieces = (int)((D.V + piece - 1) / piece);
+  L.piece = L.pieces == 1 ? D.V : rup((D.V + L.pieces - 1) / L.pieces, 256);
+  L.pieces = (int)((D.V + L.piece - 1) / L.piece);
+  L.ld = rup(L.piece, 64);
+  if (call == MAPL_XENT_FWD) {
+    L.part = c.take((size_t)(bf ? xent_partials(D.V, T) : L.pieces) * T * 8);
+    L.tgt = c.take((size_t)T * 4);
+    if (!bf) L.dl = c.take((size_t)T * L.ld * 4);
+  } else {
+    L.tok = c.take((size_t)T * 16);
+    L.hm = c.take((size_t)T * D.d * es);
+    L.dl = c.take((size_t)T * L.ld * es);
+    if (bf) {
+      // dH has few output tiles: K split over the idle CUs, at least 512 deep
+      const int64_t tiles = (D.d + 255) / 256 * ((T + 255) / 256);
+      int64_t s = tiles < 256 ? 256 / tiles : 1;
+      if (s > (L.piece + 511) / 512) s = (L.piece + 511) / 512;
+      L.kper = rup((L.piece + s - 1) / s, 64);
+      L.splits = (int)((L.piece + L.kper - 1) / L.kper);
+      if (L.splits > 1 || L.pieces > 1) L.acc = c.take((size_t)L.splits * T * D.d * 4);
+    }
+  }
+  L.total = c.off;
+  return L;
+}
+
+int check_xent(const mapl_xent_desc* D) {
+  if (!D) return fail(MAPL_E_NULL, "desc is NULL");
+  if (D->x_dtype != MAPL_BF16 && D->x_dtype != MAPL_F32)
+    return fail(MAPL_E_DTYPE, "x_dtype must be MAPL_BF16 or MAPL_F32 (got %d)", D->x_dtype);
+  if (D->dw_dtype != MAPL_F32 && !(D->dw_dtype == MAPL_BF16 && D->x_dtype == MAPL_BF16))
+    return fail(MAPL_E_DTYPE, "dw_dtype must be MAPL_F32, or MAPL_BF16 with bf16 inputs (got %d)", D->dw_dtype);
+  if (D->T < 0 || D->T > ((int64_t)1 << 22)) return fail(MAPL_E_SHAPE, "T=%lld: need 0 <= T <= 2^22", (long long)D->T);
+  if (D->V < 1 || D->V > ((int64_t)1 << 22)) return fail(MAPL_E_SHAPE, "V=%lld: need 1 <= V <= 2^22", (long long)D->V);
+  if (D->d < 64 || D->d > 16384 || D->d % 64)
+    return fail(MAPL_E_SHAPE, "d=%lld: need 64 <= d <= 16384, d %% 64 == 0", (long long)D->d);
+  return MAPL_OK;
+}
+
+int run_target_check(const mapl_xent_desc& D, const int32_t* y, int* flag, hipStream_t s) {
+  if (!debug_ids() || D.T == 0) return MAPL_OK;
+  MAPL_HIP(launch_zero_bytes(flag, 4, s));
+  MAPL_HIP(launch_xent_check(y, (int)D.T, D.V, flag, s));
+  int h = 0;
+  MAPL_HIP(hipMemcpyAsync(&h, flag, 4, hipMemcpyDeviceToHost, s));
+  MAPL_HIP(hipStreamSynchronize(s));
+  if (h) return fail(MAPL_E_RANGE, "a target is at or past V=%lld", (long long)D.V);
+  return MAPL_OK;
+}
+
+// fp32 logits of the vocabulary entries [v0, v0 + n): l [T][ld]
+GemmF32Args xent_logits_f32(const mapl_xent_desc& D, const void* H, const void* W, int64_t v0, int64_t n, float* l,
+                            int64_t ld) {
+  GemmF32Args g = gemm((int)D.T, (int)n, (int)D.d);
+  g.A = H; g.sAm = D.d; g.sAk = 1;
+  g.B = (const float*)W + v0 * D.d; g.sBk = 1; g.sBn = D.d;
+  g.C = l; g.sCm = ld; g.sCn = 1;
+  return g;
+}
+}  // namespace
+
+extern "C" size_t mapl_xent_workspace_bytes(const mapl_xent_desc* desc, int call) {
+  g_err.clear();
+  if (call != MAPL_XENT_FWD && call != MAPL_XENT_BWD) {
+    fail(MAPL_E_SHAPE, "unknown call %d", call);
+    return 0;
+  }
+  if (check_xent(desc) != MAPL_OK) return 0;
+  return xent_layout(*desc, call).total;
+}
+
+extern "C" int mapl_xent_fwd(const mapl_xent_desc* desc, const void* H, const void* W, const int32_t* targets, float* loss,
+                             float* lse, void* ws, size_t ws_bytes, void* stream) {
+  g_err.clear();
+  int st = check_xent(desc);
+  if (st) return st;
+  const mapl_xent_desc& D = *desc;
+  const int64_t T = D.T, V = D.V, d = D.d;
+  const size_t xe = esize(D.x_dtype), hb = (size_t)T * d * xe, wb = (size_t)V * d * xe, tb = (size_t)T * 4;
+  st = check_ptrs({{H, hb, "H"}, {W, wb, "W"}, {targets, tb, "targets"}, {loss, tb, "loss"}, {lse, tb, "lse"}},
+                  {{loss, tb, "loss"}, {lse, tb, "lse"}},
+                  {{H, hb, "H"}, {W, wb, "W"}, {targets, tb, "targets"}, {ws, ws_bytes, "workspace"}});
+  if (!st) st = check_ptrs({}, {{loss, tb, "loss"}}, {{lse, tb, "lse"}});
+  if (st) return st;
+  const XentLayout L = xent_layout(D, MAPL_XENT_FWD);
+  if ((st = check_ws(ws, ws_bytes, L.total))) return st;
+  hipStream_t s = (hipStream_t)stream;
+  if ((st = run_target_check(D, targets, at<int>(ws, L.flag), s))) return st;
+  if (T == 0) return MAPL_OK;
+  const XentTok a{targets, nullptr};
+  float *part = at<float>(ws, L.part), *tgt = at<float>(ws, L.tgt);
+  int np = L.pieces;
+  if (D.x_dtype == MAPL_BF16) {
+    XentGemm q{(const bf16_t*)W, d, (const bf16_t*)H, d, (int)V, (int)T, d, 0};
+    np = xent_partials(V, T);
+    LAUNCH("xent:lse", launch_xent_lse(q, a, part, tgt, s));
+  } else {
+    float* l = at<float>(ws, L.dl);
+    for (int p = 0; p < L.pieces; ++p) {
+      const int64_t v0 = p * L.piece, n = V - v0 < L.piece ? V - v0 : L.piece;
+      LAUNCH("xent:logits", launch_gemm_f32(xent_logits_f32(D, H, W, v0, n, l, L.ld), s));
+      LAUNCH("xent:lse", launch_xent_lse_f32(l, L.ld, (int)T, (int)n, (int)v0, a, part + 2 * p * T, tgt, s));
+    }
+  }
+  LAUNCH("xent:join", launch_xent_join(part, np, (int)T, a, tgt, loss, lse, s));
+  return MAPL_OK;
+}
+
+extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const void* W, const int32_t* targets,
+                             const float* lse, const float* weight, float scale, void* dH, void* dW, int accumulate_dW,
+                             void* ws, size_t ws_bytes, void* stream) {
+  g_err.clear();
+  int st = check_xent(desc);
+  if (st) return st;
+  const mapl_xent_desc& D = *desc;
+  const int64_t T = D.T, V = D.V, d = D.d;
+  const size_t xe = esize(D.x_dtype), hb = (size_t)T * d * xe, wb = (size_t)V * d * xe, tb = (size_t)T * 4;
+  const size_t dwb = (size_t)V * d * esize(D.dw_dtype);
+  if (!dH && !dW && T > 0) return fail(MAPL_E_NULL, "dH and dW are both NULL");
+  st = check_ptrs({{H, hb, "H"}, {W, wb, "W"}, {targets, tb, "targets"}, {lse, tb, "lse"}, {weight, 0, "weight"},
+                   {dH, 0, "dH"}, {dW, 0, "dW"}},
+                  {{dH, hb, "dH"}, {dW, dwb, "dW"}},
+                  {{H, hb, "H"}, {W, wb, "W"}, {targets, tb, "targets"}, {lse, tb, "lse"}, {weight, tb, "weight"},
+                   {ws, ws_bytes, "workspace"}});
+  if (!st) st = check_ptrs({}, {{dH, hb, "dH"}}, {{dW, dwb, "dW"}});
+  if (st) return st;
+  const XentLayout L = xent_layout(D, MAPL_XENT_BWD);
+  if ((st = check_ws(ws, ws_bytes, L.total))) return st;
+  hipStream_t s = (hipStream_t)stream;
+  if ((st = run_target_check(D, targets, at<int>(ws, L.flag), s))) return st;
+  if (T == 0) {
+    if (dW && !accumulate_dW) LAUNCH("xent_bwd:zero_bytes", launch_zero_bytes(dW, (int64_t)dwb, s));
+    return MAPL_OK;
+  }
+  const XentTok a{targets, weight};
+  float* tok = at<float>(ws, L.tok);
+  void* Hm = at<void>(ws, L.hm);
+  LAUNCH("xent_bwd:prep", launch_xent_prep(H, (int)xe, (int)T, (int)d, a, lse, tok, dW ? Hm : nullptr, s));
+
+  if (D.x_dtype == MAPL_BF16) {
+    bf16_t* dl = at<bf16_t>(ws, L.dl);
+    float* acc = L.acc ? at<float>(ws, L.acc) : nullptr;
+    for (int p = 0; p < L.pieces; ++p) {
+      const int64_t v0 = p * L.piece, n = V - v0 < L.piece ? V - v0 : L.piece;
+      const bf16_t* Wp = (const bf16_t*)W + v0 * d;
+      LAUNCH("xent_bwd:dl",
+             launch_xent_dl({Wp, d, (const bf16_t*)H, d, (int)n, (int)T, d, 0}, tok, (int)v0, dl, L.ld, s));
+      if (dH) {
+        XentOut o{};
+        o.ld = d;
+        o.tok = (const float4*)tok;
+        if (acc) {
+          o.out = acc; o.f32 = 1; o.add = p > 0; o.scale = 1.f; o.split_stride = T * d;
+        } else {
+          o.out = dH; o.scale = scale;
+        }
+        LAUNCH("xent_bwd:dH", launch_xent_out({Wp, d, dl, L.ld, (int)d, (int)T, n, L.kper}, 0, o, s));
+      }
+      if (dW) {
+        XentOut o{};
+        o.ld = d;
+        o.f32 = D.dw_dtype == MAPL_F32;
+        o.out = (char*)dW + (size_t)v0 * d * esize(D.dw_dtype);
+        o.add = accumulate_dW;
+        o.scale = scale;
+        LAUNCH("xent_bwd:dW", launch_xent_out({(const bf16_t*)Hm, d, dl, L.ld, (int)d, (int)n, T, 0}, 1, o, s));
+      }
+    }
+    if (dH && acc) LAUNCH("xent_bwd:sum", launch_xent_sum(acc, L.splits, (int)T, (int)d, tok, scale, (bf16_t*)dH, s));
+    return MAPL_OK;
+  }
+
+  // ---------------- fp32 path: the vector loads take extents that are
+  // multiples of 4; a piece's last one to three entries go on their own
+  float* l = at<float>(ws, L.dl);
+  for (int p = 0; p < L.pieces; ++p) {
+    const int64_t v0 = p * L.piece, n = V - v0 < L.piece ? V - v0 : L.piece;
+    LAUNCH("xent_bwd:logits", launch_gemm_f32(xent_logits_f32(D, H, W, v0, n, l, L.ld), s));
+    LAUNCH("xent_bwd:dl", launch_xent_dl_f32(l, L.ld, (int)T, (int)n, (int)v0, lse, a, scale, s));
+    for (int64_t u0 = 0; u0 < n; u0 += n & ~(int64_t)3 ? n & ~(int64_t)3 : n) {
+      const int64_t m = u0 == 0 && n >= 4 ? n & ~(int64_t)3 : n - u0;
+      const float* Wp = (const float*)W + (v0 + u0) * d;
+      if (dH) {
+        GemmF32Args g = gemm((int)T, (int)d, (int)m);
+        g.A = l + u0; g.sAm = L.ld; g.sAk = 1;
+        g.B = Wp; g.sBk = d; g.sBn = 1;
+        g.C = dH; g.sCm = d; g.sCn = 1;
+        if (v0 + u0 > 0) { g.Cin = (const float*)dH; g.sCinm = d; g.sCinn = 1; g.beta = 1.f; }
+        LAUNCH("xent_bwd:dH", launch_gemm_f32(g, s));
+      }
+      if (dW) {
+        GemmF32Args g = gemm((int)m, (int)d, (int)T);
+        float* out = (float*)dW + (v0 + u0) * d;
+        g.A = l + u0; g.sAm = 1; g.sAk = L.ld;
+        g.B = Hm; g.sBk = d; g.sBn = 1;
+        g.C = out; g.sCm = d; g.sCn = 1;
+        if (accumulate_dW) { g.Cin = out; g.sCinm = d; g.sCinn = 1; g.beta = 1.f; }
+        LAUNCH("xent_bwd:dW", launch_gemm_f32(g, s));
+      }
+    }
+  }
+  if (dH) LAUNCH("xent_bwd:mask", launch_xent_zero_rows((float*)dH, (int)T, (int)d, a, s));
+  return MAPL_OK;
 }
 
 // ---------------------------------------------------------------- tracing API

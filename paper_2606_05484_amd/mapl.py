@@ -20,6 +20,7 @@ F32, BF16, U8, U16 = 0, 1, 2, 3
 AMBIENT, COORD = 0, 1
 CALL_ENCODE, CALL_DECODE, CALL_DECODE_BWD, CALL_ENCODE_BWD, CALL_STIEFEL = range(5)
 SENDER, RECEIVER = 0, 1
+XENT_FWD, XENT_BWD = 0, 1
 _DT = {"f32": F32, "bf16": BF16, "u8": U8, "u16": U16}
 _SPACE = {"ambient": AMBIENT, "coord": COORD}
 
@@ -35,6 +36,11 @@ class CodecDesc(ctypes.Structure):
                 ("k", ctypes.c_int64), ("anchor_space", ctypes.c_int32), ("L", ctypes.c_int32),
                 ("K", ctypes.c_int32), ("x_dtype", ctypes.c_int32), ("ab_dtype", ctypes.c_int32),
                 ("code_dtype", ctypes.c_int32), ("group_dim", ctypes.c_int32)]
+
+
+class XentDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("d", ctypes.c_int64), ("V", ctypes.c_int64), ("x_dtype", ctypes.c_int32),
+                ("dw_dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -55,6 +61,14 @@ _SIG = {
     "mapl_anchor_bwd_workspace_bytes": [ctypes.POINTER(CodecDesc), ctypes.c_int],
     "mapl_grad_dequantize": [ctypes.c_int64, ctypes.c_int64] + [ctypes.c_int32] * 3 + [_P, _P, ctypes.c_int32,
                                                                                         _P, _P],
+    "mapl_ckpt_pack": [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32] + [_P] * 4,
+    "mapl_ckpt_unpack": [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32] + [_P] * 4,
+    "mapl_ckpt_encode_bwd": [ctypes.POINTER(CodecDesc)] + [_P] * 9 + [ctypes.c_int, _P, ctypes.c_size_t, _P],
+    "mapl_ckpt_encode_bwd_workspace_bytes": [ctypes.POINTER(CodecDesc)],
+    "mapl_xent_fwd": [ctypes.POINTER(XentDesc)] + [_P] * 5 + [_P, ctypes.c_size_t, _P],
+    "mapl_xent_bwd": [ctypes.POINTER(XentDesc)] + [_P] * 5 + [ctypes.c_float] + [_P] * 2 + [ctypes.c_int, _P,
+                                                                                          ctypes.c_size_t, _P],
+    "mapl_xent_workspace_bytes": [ctypes.POINTER(XentDesc), ctypes.c_int],
     "mapl_stiefel_step": [ctypes.c_int64] * 3 + [_P] * 3 + [ctypes.c_float, ctypes.c_float, ctypes.c_int,
                                                             ctypes.c_int, _P, ctypes.c_size_t, _P],
     "mapl_workspace_bytes": [ctypes.POINTER(CodecDesc), ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
@@ -65,7 +79,8 @@ _SIG = {
     "mapl_profile_report": [ctypes.c_char_p, ctypes.c_size_t],
 }
 _RES = {"mapl_workspace_bytes": ctypes.c_size_t, "mapl_decode_bwd_q_workspace_bytes": ctypes.c_size_t,
-        "mapl_anchor_bwd_workspace_bytes": ctypes.c_size_t,
+        "mapl_anchor_bwd_workspace_bytes": ctypes.c_size_t, "mapl_ckpt_encode_bwd_workspace_bytes": ctypes.c_size_t,
+        "mapl_xent_workspace_bytes": ctypes.c_size_t,
         "mapl_last_error": ctypes.c_char_p}
 EXPORTS = tuple(_SIG)
 
@@ -212,6 +227,66 @@ def encode_bwd(D, dZ, X, ids, U, A_s, B_s, dX, dU, accumulate_dU, ws, ws_bytes=N
     wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
     _check(lib().mapl_encode_bwd(ctypes.byref(D), _ptr(dZ), _ptr(X), _ptr(ids), _ptr(U), _ptr(A_s), _ptr(B_s),
                                  _ptr(dX), _ptr(dU), int(accumulate_dU), _ptr(ws), wb, _stream(stream)))
+
+
+CKPT_BLOCK = 32  # tokens of one channel that share a scale
+
+
+def ckpt_shapes(T, d):
+    """Shapes of a checkpoint's int8 values and uint8 exponents."""
+    nb = -(-T // CKPT_BLOCK)
+    return (nb, d, CKPT_BLOCK), (nb, d)
+
+
+def ckpt_pack(T, d, X, q, e, x_dtype="bf16", stream=None):
+    """Keep X [T, d] in 8 bits: q int8 and e uint8 of ckpt_shapes(T, d)."""
+    _check(lib().mapl_ckpt_pack(T, d, _DT.get(x_dtype, x_dtype), _ptr(X), _ptr(q), _ptr(e), _stream(stream)))
+
+
+def ckpt_unpack(T, d, q, e, X, x_dtype="bf16", stream=None):
+    """The values that a checkpoint stands for."""
+    _check(lib().mapl_ckpt_unpack(T, d, _DT.get(x_dtype, x_dtype), _ptr(q), _ptr(e), _ptr(X), _stream(stream)))
+
+
+def ckpt_encode_bwd(D, dZ, q, e, ids, U, A_s, B_s, dX, dU, accumulate_dU, ws, ws_bytes=None, stream=None):
+    """encode_bwd with X read from its 8-bit checkpoint."""
+    wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
+    _check(lib().mapl_ckpt_encode_bwd(ctypes.byref(D), _ptr(dZ), _ptr(q), _ptr(e), _ptr(ids), _ptr(U), _ptr(A_s),
+                                      _ptr(B_s), _ptr(dX), _ptr(dU), int(accumulate_dU), _ptr(ws), wb,
+                                      _stream(stream)))
+
+
+def ckpt_encode_bwd_workspace_bytes(D):
+    n = lib().mapl_ckpt_encode_bwd_workspace_bytes(ctypes.byref(D))
+    if n == 0 and last_error():
+        raise MaplError(-2, last_error())
+    return n
+
+
+def xent_desc(T, d, V, x_dtype="bf16", dw_dtype="f32"):
+    """Build a mapl_xent_desc (dw_dtype: the type of dW)."""
+    return XentDesc(T, d, V, _DT.get(x_dtype, x_dtype), _DT.get(dw_dtype, dw_dtype))
+
+
+def xent_workspace_bytes(D, call):
+    n = lib().mapl_xent_workspace_bytes(ctypes.byref(D), call)
+    if n == 0 and last_error():
+        raise MaplError(-2, last_error())
+    return n
+
+
+def xent_fwd(D, H, W, targets, loss, lse, ws, ws_bytes=None, stream=None):
+    """Cross entropy of the logits H W^T: loss and log-sum-exp of every token."""
+    wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
+    _check(lib().mapl_xent_fwd(ctypes.byref(D), _ptr(H), _ptr(W), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(ws), wb,
+                               _stream(stream)))
+
+
+def xent_bwd(D, H, W, targets, lse, weight, scale, dH, dW, accumulate_dW, ws, ws_bytes=None, stream=None):
+    """Its gradient: dH, and dW (added to with accumulate_dW); either may be None."""
+    wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
+    _check(lib().mapl_xent_bwd(ctypes.byref(D), _ptr(H), _ptr(W), _ptr(targets), _ptr(lse), _ptr(weight), float(scale),
+                               _ptr(dH), _ptr(dW), int(accumulate_dW), _ptr(ws), wb, _stream(stream)))
 
 
 def stiefel_step(P, d, r, U, G, M, lr, beta, lmo_steps, retract_steps, ws, ws_bytes=None, stream=None):

@@ -188,8 +188,8 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Epi&& epi) 
       if constexpr (Cfg::PT) np = (uint32_t)rows * (uint32_t)g.P.ld * 2u - l_np;
       if constexpr (Cfg::QT) nq = (uint32_t)rows * (uint32_t)g.Q.ld * 2u - l_nq;
     }
-    rp = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(l_p), 0, np, 0x00020000);
-    rq = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(l_q), 0, nq, 0x00020000);
+    rp = uniform_rsrc(l_p, np);
+    rq = uniform_rsrc(l_q, nq);
   };
   auto issue = [&](auto b0c, auto b1c) {
     constexpr int B0 = decltype(b0c)::value, B1 = decltype(b1c)::value;

@@ -169,6 +169,17 @@ __device__ __forceinline__ void reg_pin(u32x4 (&v)[N]) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
 
+// A buffer resource whose base and size the compiler knows to be uniform.
+// (Uniform values that passed through vector registers -- a division, a clamp
+// -- would put a loop over the lanes around every load of the resource.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void* base, uint32_t bytes) {
+  const uint64_t p = (uint64_t)(uintptr_t)base;
+  const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
+  const uint64_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(uintptr_t)(lo | hi << 32), 0,
+                                           (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+}
+
 // Chunk swizzle of token-major tiles: chunk c of row t is stored at
 // c ^ wg_sw(t, cpr); it stays inside the row for every cpr >= 8.
 __device__ __forceinline__ int wg_sw(int row, int cpr) { return (4 * (row & 3)) & (cpr - 1); }

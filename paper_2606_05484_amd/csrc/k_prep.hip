@@ -336,6 +336,35 @@ __global__ void k_transpose_into(const void* __restrict__ src, int src_f32, int 
   transpose_tile(blockIdx.x, blockIdx.y, src, src_f32, rows, cols, lds, scale, dst, ldd, off);
 }
 __global__ void k_assemble(AssembleArgs a) { assemble_block(blockIdx.x, a); }
+// Gathered rows in the weight gradient's operand order, out [ceil(T/32)][k][32]
+// (tokens past T are zeros): one thread per 16 tokens of a block and two
+// columns, its rows' 4-byte pieces loaded at once.
+__device__ __forceinline__ void gather_blocks_block(int bx, const bf16_t* __restrict__ A, int k,
+                                                    const int32_t* __restrict__ ids, int V, int T,
+                                                    bf16_t* __restrict__ out) {
+  const int64_t e = (int64_t)bx * 256 + threadIdx.x;
+  const int cols = k / 2;
+  const int64_t run = e / cols;  // 16-token run
+  const int c = (int)(e - run * cols);
+  if (run >= 2 * (((int64_t)T + 31) / 32)) return;
+  const int t0 = (int)(run * 16);
+  uint32_t v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    v[i] = t0 + i < T ? *(const uint32_t*)(A + (int64_t)clamp_id(ids[t0 + i], V) * k + 2 * c) : 0u;
+  uint4* o = (uint4*)(out + ((run >> 1) * k + 2 * c) * 32 + 16 * (run & 1));
+  uint32_t lo[8], hi[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo[i] = (v[2 * i] & 0xFFFFu) | (v[2 * i + 1] << 16);
+    hi[i] = (v[2 * i] >> 16) | (v[2 * i + 1] & 0xFFFF0000u);
+  }
+  o[0] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  o[1] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
+  o[4] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  o[5] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+}
+
 __global__ void k_gather_rows_bf16(const bf16_t* __restrict__ A, int k, const int32_t* __restrict__ ids, int V,
                                    int T, bf16_t* __restrict__ out) {
   gather_rows_block(blockIdx.x, A, k, ids, V, T, out);
@@ -420,6 +449,7 @@ __global__ __launch_bounds__(256) void k_prep_batch(PrepBatch batch) {
     case PJ_ASSEMBLE: assemble_block(b, j.asm_args); break;
     case PJ_ASSEMBLE_SUM: assemble_sum_block(b, j.asm_args); break;
     case PJ_GATHER: gather_rows_block(b, j.A, j.k, j.ids, j.V, j.T, j.out); break;
+    case PJ_GATHER_BLOCKS: gather_blocks_block(b, j.A, j.k, j.ids, j.V, j.T, j.out); break;
     case PJ_SMALL_GEMM: small_gemm_tile(b % j.gx, b / j.gx, j); break;
     default: break;
   }
@@ -514,6 +544,14 @@ PrepJob prep_job_assemble(const AssembleArgs& a) {
   return j;
 }
 
+PrepJob prep_job_gather_blocks(const bf16_t* A, int k, const int32_t* ids, int V, int T, bf16_t* out) {
+  PrepJob j{};
+  j.kind = PJ_GATHER_BLOCKS;
+  j.A = A; j.k = k; j.ids = ids; j.V = V; j.T = T; j.out = out;
+  j.blocks = T > 0 ? (int)((((int64_t)T + 31) / 32 * k + 255) / 256) : 0;
+  return j;
+}
+
 PrepJob prep_job_gather(const bf16_t* A, int k, const int32_t* ids, int V, int T, bf16_t* out) {
   PrepJob j{};
   j.kind = PJ_GATHER;
@@ -546,7 +584,7 @@ hipError_t launch_prep_batch(const PrepJob* jobs, int n, hipStream_t s) {
         (jobs[i].asm_args.r % 8 || jobs[i].asm_args.ldo % 8 ||
                                         (jobs[i].asm_args.A != nullptr && jobs[i].asm_args.k % 8)))
       return hipErrorInvalidValue;
-    if (jobs[i].kind == PJ_GATHER && jobs[i].k % 8) return hipErrorInvalidValue;
+    if ((jobs[i].kind == PJ_GATHER || jobs[i].kind == PJ_GATHER_BLOCKS) && jobs[i].k % 8) return hipErrorInvalidValue;
     b.job[b.n++] = jobs[i];
     total += jobs[i].blocks;
   }

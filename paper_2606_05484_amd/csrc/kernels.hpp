@@ -181,7 +181,7 @@ hipError_t launch_assemble(const AssembleArgs& a, hipStream_t s);
 // ---------------------------------------------------------------- batched preparation
 // Independent preparation jobs of one call issued as a single launch
 // (launch_prep_batch); each job behaves like the corresponding launcher.
-enum { PJ_PREP_U = 1, PJ_TRANSPOSE, PJ_CODEBOOK, PJ_ASSEMBLE, PJ_GATHER, PJ_SMALL_GEMM, PJ_ASSEMBLE_SUM };
+enum { PJ_PREP_U = 1, PJ_TRANSPOSE, PJ_CODEBOOK, PJ_ASSEMBLE, PJ_GATHER, PJ_SMALL_GEMM, PJ_ASSEMBLE_SUM, PJ_GATHER_BLOCKS };
 struct PrepJob {
   int kind, blocks, gx;
   // PJ_PREP_U
@@ -192,7 +192,7 @@ struct PrepJob {
   const float* C; int L, K; bf16_t* Cb; float* meta; float* cscale;
   // PJ_ASSEMBLE, PJ_ASSEMBLE_SUM (codeword sums only: L <= 2, no anchor columns)
   AssembleArgs asm_args;
-  // PJ_GATHER
+  // PJ_GATHER, PJ_GATHER_BLOCKS (out [ceil(T/32)][k][32], the operand order of launch_wgrad8)
   const bf16_t* A; int k; const int32_t* ids; int V, T; bf16_t* out;
   // PJ_SMALL_GEMM: dst[c*ldd + off + i] = bf16(scale * sum_j P[i][j] bf16(Q(j, c))),
   // Q(j, c) = Q[j*ldq + c] (qt = 0) or Q[c*ldq + j] (qt = 1)
@@ -209,6 +209,7 @@ PrepJob prep_job_transpose(const void* src, int src_f32, int rows, int cols, int
 PrepJob prep_job_codebook(const float* C, int L, int K, int r, bf16_t* Cb, float* meta, float* scale);
 PrepJob prep_job_assemble(const AssembleArgs& a);
 PrepJob prep_job_gather(const bf16_t* A, int k, const int32_t* ids, int V, int T, bf16_t* out);
+PrepJob prep_job_gather_blocks(const bf16_t* A, int k, const int32_t* ids, int V, int T, bf16_t* out);
 PrepJob prep_job_small_gemm(const bf16_t* P, int64_t ldp, const float* Q, int64_t ldq, int qt, int M, int N,
                             int Kd, float scale, bf16_t* dst, int64_t ldd, int off);
 hipError_t launch_prep_batch(const PrepJob* jobs, int n, hipStream_t s);
@@ -342,6 +343,19 @@ hipError_t launch_anchor_segsum(const AnchorSegArgs& a, hipStream_t s);
 // (fp32 or bf16), and back (see k_ckpt.hip for the format).
 hipError_t launch_ckpt_pack(const void* X, int f32, int64_t T, int d, void* q, uint8_t* e, hipStream_t s);
 hipError_t launch_ckpt_unpack(const void* q, const uint8_t* e, int64_t T, int d, void* X, int f32, hipStream_t s);
+
+// part[s][m][n] = sum over the tokens t of split s of P[t][m] Q[t][n]: for m < d
+// P is the checkpoint (q, e) of X [T][d], for d <= m < d + ka the bf16 rows
+// ga [ceil(T/32)][ka][32] (ka % 16 == 0, may be 0); Q [T][ldq] bf16, N % 64 == 0 columns,
+// tokens_per_split % 64 == 0, no split empty; part [splits][d + ka][N].
+struct Wgrad8Args {
+  const void* q; const uint8_t* e; int d;
+  const bf16_t* ga; int ka;
+  const bf16_t* Q; int64_t ldq;
+  int64_t T; int N, splits, tokens_per_split;
+  float* part;
+};
+hipError_t launch_wgrad8(const Wgrad8Args& g, hipStream_t s);
 
 // ---------------------------------------------------------------- vocabulary cross entropy
 // Products of bf16 operands, C(m, n) = sum_k P(m, k) Q(n, k): M x N, K split

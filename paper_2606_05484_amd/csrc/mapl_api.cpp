@@ -160,6 +160,7 @@ struct Layout {
   size_t total = 0;
   size_t w = 0, w2 = 0, z0 = 0, cb = 0, cn2 = 0, cnr = 0, stats = 0, flag = 0;
   size_t ahat = 0, part = 0, wsum = 0, ga = 0, bu = 0, zh = 0, z2 = 0, bt = 0, wt = 0;
+  size_t x = 0;
   int64_t kp = 0, kw = 0;
   SplitPlan sp{1, 64};
 };
@@ -175,7 +176,10 @@ struct GradQ {
   void* codes;
 };
 
-Layout layout(const mapl_codec_desc& D, int call, const GradQ* q = nullptr) {
+// ck: mapl_ckpt_encode_bwd.  On the bf16 path its weight gradient reads the
+// checkpoint, and the gathered anchors in the same blocks of 32 tokens; the
+// fp32 path unpacks X into the workspace.
+Layout layout(const mapl_codec_desc& D, int call, const GradQ* q = nullptr, bool ck = false) {
   Layout Lo;
   Carve c;
   c.take(0);
@@ -220,10 +224,10 @@ Layout layout(const mapl_codec_desc& D, int call, const GradQ* q = nullptr) {
         Lo.w2 = c.take((size_t)d * r * 2);
         const int mg = (amb && k > 0) ? (int)k : 0;
         Lo.sp = plan_splits(T, (int)d, mg, (int)r);
-        Lo.part = c.take((size_t)Lo.sp.splits * (wgrad_row_offset((int)d) + mg) * r * 4);
+        Lo.part = c.take((size_t)Lo.sp.splits * ((ck ? d : wgrad_row_offset((int)d)) + mg) * r * 4);
         if (mg) {
           Lo.wsum = c.take((size_t)k * r * 4);   // a_s^T dZ
-          Lo.ga = c.take((size_t)T * k * 2);     // a_s = A_s[ids], token-major bf16
+          Lo.ga = c.take((size_t)(ck ? rup(T, 32) : T) * k * 2);  // a_s = A_s[ids], bf16
         }
         break;
       }
@@ -244,6 +248,7 @@ Layout layout(const mapl_codec_desc& D, int call, const GradQ* q = nullptr) {
         if (k > 0 && amb) {
           Lo.wsum = c.take((size_t)k * r * 4);
         }
+        if (ck) Lo.x = c.take((size_t)T * d * 4);
         break;
     }
   }
@@ -850,15 +855,6 @@ namespace {
 size_t ckpt_q_bytes(int64_t T, int64_t d) { return (size_t)((T + 31) / 32) * 32 * d; }
 size_t ckpt_e_bytes(int64_t T, int64_t d) { return (size_t)((T + 31) / 32) * d; }
 
-// The workspace of encode_bwd from a checkpoint: encode_bwd's, then X.
-size_t ckpt_x_offset(const mapl_codec_desc& D) { return layout(D, MAPL_CALL_ENCODE_BWD).total; }
-size_t ckpt_ws_bytes(const mapl_codec_desc& D) {
-  Carve c;
-  c.take(ckpt_x_offset(D));
-  c.take((size_t)D.T * D.d * esize(D.x_dtype));
-  return c.off;
-}
-
 // mapl_encode_bwd on X, or (ck) mapl_ckpt_encode_bwd on X's checkpoint (q, e).
 int encode_bwd(const mapl_codec_desc* desc, const void* dZ, const void* X, bool ck, const int8_t* q, const uint8_t* e,
                const int32_t* ids, const float* U, const void* A_s, const void* B_s, void* dX, float* dU,
@@ -886,20 +882,14 @@ int encode_bwd(const mapl_codec_desc* desc, const void* dZ, const void* X, bool 
     const uintptr_t a0 = (uintptr_t)dX, a1 = a0 + T * d * xe, b0 = (uintptr_t)dU, b1 = b0 + d * r * 4;
     if (a0 < b1 && b0 < a1) return fail(MAPL_E_ALIAS, "output dX overlaps output dU");
   }
-  const Layout Lo = layout(D, MAPL_CALL_ENCODE_BWD);
-  if ((st = check_ws(ws, ws_bytes, ck ? ckpt_ws_bytes(D) : Lo.total))) return st;
+  const Layout Lo = layout(D, MAPL_CALL_ENCODE_BWD, nullptr, ck);
+  if ((st = check_ws(ws, ws_bytes, Lo.total))) return st;
   hipStream_t s = (hipStream_t)stream;
   if (need_anchor && (st = run_id_check(ids, T, D.V, ws, Lo, s))) return st;
   if (T == 0) {
     if (!accumulate_dU) LAUNCH("enc_bwd:zero_bytes", launch_zero_bytes(dU, d * r * 4, s));
     return MAPL_OK;
   }
-  if (ck) {
-    void* Xq = at<char>(ws, ckpt_x_offset(D));
-    LAUNCH("enc_bwd:unpack", launch_ckpt_unpack(q, e, T, (int)d, Xq, D.x_dtype == MAPL_F32, s));
-    X = Xq;
-  }
-
   if (D.x_dtype == MAPL_BF16) {
     // one launch: Ub = U~ and the gathered sender anchors a_s
     bf16_t* Ub = at<bf16_t>(ws, Lo.w2);
@@ -907,7 +897,8 @@ int encode_bwd(const mapl_codec_desc* desc, const void* dZ, const void* X, bool 
     PrepJob jobs[2];
     int nj = 0;
     jobs[nj++] = prep_job_u(U, (int)d, (int)r, Ub, r, nullptr, 0);
-    if (need_anchor) jobs[nj++] = prep_job_gather((const bf16_t*)A_s, (int)k, ids, (int)D.V, (int)T, ga);
+    if (need_anchor)
+      jobs[nj++] = (ck ? prep_job_gather_blocks : prep_job_gather)((const bf16_t*)A_s, (int)k, ids, (int)D.V, (int)T, ga);
     LAUNCH("enc_bwd:prep", launch_prep_batch(jobs, nj, s));
     TnArgs g{};
     g.A = (const bf16_t*)dZ; g.lda = r; g.Ka = (int)r;
@@ -915,31 +906,41 @@ int encode_bwd(const mapl_codec_desc* desc, const void* dZ, const void* X, bool 
     g.M = (int)T; g.N = (int)d;
     g.out = dX; g.ldo = d; g.out_f32 = 0;
     LAUNCH("enc_bwd:gemm_tn", launch_gemm_tn(g, s));
-    WgradArgs w{};
-    w.Pa = (const bf16_t*)X; w.ldp = d; w.Ma = (int)d;
-    if (need_anchor) {
-      w.Tg = ga; w.Mg = (int)k;
+    const int mg = need_anchor ? (int)k : 0;
+    const int64_t mao = ck ? d : wgrad_row_offset((int)d);
+    const int64_t stride = (mao + mg) * r;
+    float* part = at<float>(ws, Lo.part);
+    if (ck) {
+      Wgrad8Args w{q, e, (int)d, ga, mg, (const bf16_t*)dZ, r, T, (int)r, Lo.sp.splits, Lo.sp.tps, part};
+      LAUNCH("enc_bwd:wgrad8", launch_wgrad8(w, s));
+    } else {
+      WgradArgs w{};
+      w.Pa = (const bf16_t*)X; w.ldp = d; w.Ma = (int)d;
+      w.Tg = ga; w.Mg = mg;
+      w.Q = (const bf16_t*)dZ; w.ldq = r;
+      w.T = (int)T; w.N = (int)r; w.splits = Lo.sp.splits; w.tokens_per_split = Lo.sp.tps;
+      w.part = part;
+      LAUNCH("enc_bwd:wgrad", launch_wgrad(w, s));
     }
-    w.Q = (const bf16_t*)dZ; w.ldq = r;
-    w.T = (int)T; w.N = (int)r; w.splits = Lo.sp.splits; w.tokens_per_split = Lo.sp.tps;
-    w.part = at<float>(ws, Lo.part);
-    const int64_t mao = wgrad_row_offset((int)d);
-    const int64_t stride = (mao + w.Mg) * r;
-    LAUNCH("enc_bwd:wgrad", launch_wgrad(w, s));
     if (need_anchor) {
       // dU = sum of the partials - B_s^T (a_s^T dZ); a_s^T dZ is summed first
       // from the anchor rows of the partials
       float* Wa = at<float>(ws, Lo.wsum);
-      LAUNCH("enc_bwd:anchor_reduce", launch_reduce_splits(w.part + mao * r, w.splits, (int)k, (int)r, stride, Wa, 0, s));
-      LAUNCH("enc_bwd:reduce_corr", launch_reduce_dU(w.part, w.splits, stride, (int)d, (int)r, dU, accumulate_dU,
+      LAUNCH("enc_bwd:anchor_reduce", launch_reduce_splits(part + mao * r, Lo.sp.splits, (int)k, (int)r, stride, Wa, 0, s));
+      LAUNCH("enc_bwd:reduce_corr", launch_reduce_dU(part, Lo.sp.splits, stride, (int)d, (int)r, dU, accumulate_dU,
                                                      (const bf16_t*)B_s, Wa, (int)k, s));
     } else {
-      LAUNCH("enc_bwd:reduce", launch_reduce_splits(w.part, w.splits, (int)d, (int)r, stride, dU, accumulate_dU, s));
+      LAUNCH("enc_bwd:reduce", launch_reduce_splits(part, Lo.sp.splits, (int)d, (int)r, stride, dU, accumulate_dU, s));
     }
     return MAPL_OK;
   }
 
   // ---------------- fp32 path
+  if (ck) {
+    float* Xq = at<float>(ws, Lo.x);
+    LAUNCH("enc_bwd:unpack", launch_ckpt_unpack(q, e, T, (int)d, Xq, 1, s));
+    X = Xq;
+  }
   {
     GemmF32Args g = gemm((int)T, (int)d, (int)r);
     g.A = dZ; g.sAm = r; g.sAk = 1;
@@ -1485,7 +1486,7 @@ extern "C" int mapl_ckpt_unpack(int64_t T, int64_t d, int32_t x_dtype, const int
 extern "C" size_t mapl_ckpt_encode_bwd_workspace_bytes(const mapl_codec_desc* desc) {
   g_err.clear();
   if (check_desc(desc) != MAPL_OK) return 0;
-  return ckpt_ws_bytes(*desc);
+  return layout(*desc, MAPL_CALL_ENCODE_BWD, nullptr, true).total;
 }
 
 extern "C" int mapl_ckpt_encode_bwd(const mapl_codec_desc* desc, const void* dZ, const int8_t* q, const uint8_t* e,

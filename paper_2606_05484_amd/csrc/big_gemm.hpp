@@ -1,6 +1,12 @@
 // The products of the vocabulary's cross entropy: C(m, n) = sum_k P(m, k) Q(n, k)
 // on bf16 operands with fp32 accumulation, in tiles of one workgroup per CU.
 // Device code; included by the kernel sources only.
+//
+// What bounds it: at 256 x 256 tiles the matrix units are busy 70 % of the
+// time and the clock has fallen to 1.95 GHz, i.e. the card's power.  Hence
+// the 16 x 16 x 32 instruction (half of the 32 x 32 x 16 one's accumulator
+// traffic per product: 2048 x 32000 x 8192 942 -> 895 us), the XCD-blocked
+// tile order and no operand copied twice.
 #pragma once
 #include "common.hpp"
 #include "kernels.hpp"
@@ -12,17 +18,17 @@ namespace {
 typedef __attribute__((address_space(3))) void* bg_lds_ptr;
 
 // One operand X(row, k): rows contiguous along k (X + row ld + k), or (TR)
-// along the rows (X + k ld + row).  `rows` counts the valid rows where they
-// are k-contiguous; in either form what lies past the last valid row or past
-// k's end reads as zero, and under TR columns past the matrix read whatever
-// follows in memory (never past the last k-row): they reach only outputs
-// that the caller does not store.
+// along the rows (X + k ld + row).  What lies past the last valid row of a
+// k-contiguous operand, or past k's end under TR, reads as zero; a k-contiguous operand has
+// k's range up to a multiple of 64 readable.  Under TR the columns past
+// the matrix are whatever follows in memory (never past the last k-row):
+// they reach only outputs that the caller does not store.
 struct BgMat {
   const bf16_t* p;
   int64_t ld;
 };
 
-// m x n output, k-range K in `splits` runs of `kper` (a multiple of 64).
+// M x N output, k-range K in `splits` runs of `kper` (a multiple of 64).
 struct BgShape {
   BgMat P, Q;
   int M, N;
@@ -31,14 +37,16 @@ struct BgShape {
   int mt, nt;  // tiles
 };
 
+// WVM x WVN waves of 16 FM x 16 FN outputs each; square tiles.
 template <int WVM_, int WVN_, int FM_, int FN_, bool PT_, bool QT_>
 struct BgCfg {
   static constexpr int WVM = WVM_, WVN = WVN_, FM = FM_, FN = FN_;
   static constexpr bool PT = PT_, QT = QT_;
   static constexpr int NW = WVM * WVN, THREADS = 64 * NW;
-  static constexpr int BM = 32 * FM * WVM, BN = 32 * FN * WVN, BK = 64;
-  static constexpr int PBYTES = BM * BK * 2, QBYTES = BN * BK * 2, STAGE = PBYTES + QBYTES;
-  static constexpr int PL = PBYTES / 1024 / NW, QL = QBYTES / 1024 / NW, LOADS = PL + QL;
+  static constexpr int BM = 16 * FM * WVM, BN = 16 * FN * WVN, BK = 64;
+  static constexpr int PANEL = BM * BK * 2, SMEM = 5 * PANEL;
+  static constexpr int LOADS = PANEL / 1024 / NW;  // 1 KiB direct-to-LDS blocks per wave and panel
+  static_assert(BM == BN, "P and Q panels share a ring of slots");
 };
 
 template <int OFF>
@@ -55,27 +63,28 @@ __device__ __forceinline__ u32x2 bg_read_tr(uint32_t addr) {
   return r;
 }
 
-// A panel of ROWS operand rows x 64 k in LDS and its fragments.
+// A panel of ROWS operand rows x 64 k in LDS and its fragments (16 rows x 32
+// k: lane l row l % 16, k 8 (l / 16) .. +7).
 //   k-contiguous: 128 B per row, 16 B chunk c of row r at c ^ ((r >> 1) & 7);
-//   TR: ROWS 2 B per k-row, chunk c of k-row r at c ^ (4 (r & 3)) (wg_sw).
-// base[]: the lane's fragment addresses (k-contiguous: one per 16-deep
-// k-step; TR: one per i & 3, the XOR acting on the fragment's number).
-template <int ROWS, int F, bool TR>
+//   TR: ROWS 2 B per k-row, chunk c of k-row r at c ^ (4 (r & 3)) (wg_sw), read
+//   transposed (see tr_frag).
+// base[]: the lane's fragment addresses (k-contiguous: one per 32-deep
+// k-step; TR: one per fragment number (i / 2) & 3, which the XOR acts on).
+template <int ROWS, bool TR>
 struct BgPanel {
-  static constexpr int NB = 4;
+  static constexpr int NB = TR ? 4 : 2;
   uint32_t base[NB];
   __device__ __forceinline__ void init(uint32_t lds, int row0, int lane) {
     if constexpr (!TR) {
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
-        base[kk] = lds + (uint32_t)((row0 + (lane & 31)) * 128 + 16 * ((2 * kk + (lane >> 5)) ^ (((lane & 31) >> 1) & 7)));
+      for (int kk = 0; kk < 2; ++kk)
+        base[kk] = lds + (uint32_t)((row0 + (lane & 15)) * 128 + 16 * ((4 * kk + (lane >> 4)) ^ ((lane & 15) >> 1)));
     } else {
-      const int g = lane >> 4, sidx = lane & 15, j = sidx >> 2, q = sidx & 3;
-      const int k = 8 * (g >> 1) + j;
+      const int j = (lane & 15) >> 2, q = lane & 3, k = 8 * (lane >> 4) + j;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int col = row0 + 16 * (g & 1) + 4 * q;
-        base[i] = lds + (uint32_t)(k * (ROWS * 2) + 16 * (((col >> 3) + 4 * i) ^ (4 * j)) + 2 * (col & 7));
+        const int col = row0 + 32 * i + 4 * q;
+        base[i] = lds + (uint32_t)(k * (ROWS * 2) + 16 * ((col >> 3) ^ (4 * j)) + 2 * (col & 7));
       }
     }
   }
@@ -86,10 +95,11 @@ struct BgPanel {
   template <int KK, int I>
   __device__ __forceinline__ void read(u32x4& r) const {
     if constexpr (!TR) {
-      bg_read<I * 32 * 128>(r, base[KK]);
+      bg_read<I * 16 * 128>(r, base[KK]);
     } else {
-      const u32x2 a = bg_read_tr<KK * 16 * ROWS * 2 + (I >> 2) * 256>(base[I & 3]);
-      const u32x2 b = bg_read_tr<(KK * 16 + 4) * ROWS * 2 + (I >> 2) * 256>(base[I & 3]);
+      constexpr int X = KK * 32 * ROWS * 2 + (I >> 3) * 256 + (I & 1) * 32;
+      const u32x2 a = bg_read_tr<X>(base[(I >> 1) & 3]);
+      const u32x2 b = bg_read_tr<X + 4 * ROWS * 2>(base[(I >> 1) & 3]);
       r = u32x4{a.x, a.y, b.x, b.y};
     }
   }
@@ -136,20 +146,23 @@ __device__ __forceinline__ BgTile bg_tile(const BgShape& g, int item) {
 
 // Every tile of this workgroup in turn: item = round gridDim + place, places
 // dealt so that each XCD's workgroups hold consecutive items (gridDim a
-// multiple of 8).  epi(acc, tile) takes a finished tile's accumulators:
-// acc[i][j] element e of lane l is C(m, n) at m = tile.m BM + wave's first row +
-// 32 i + acc_row(e, l), n = tile.n BN + wave's first column + 32 j + l % 32.
-// smem: 2 Cfg::STAGE bytes.
+// multiple of 8).  Before a tile's last products pre(tile, wm, wn) may request
+// what its epilogue reads; epi(acc, tile, wm, wn) takes the finished
+// accumulators: acc[i][j][e] of lane l is C(m, n) at m = tile.m BM + 16 (wm FM + i)
+// + 4 (l / 16) + e, n = tile.n BN + 16 (wn FN + j) + l % 16.
+// smem: Cfg::SMEM bytes.
 //
-// Two stages of 64 k.  A stage's products run in four k-steps of 16 whose
-// fragments are read one k-step ahead; before the last k-step of stage s every
-// wave has its last fragments of s, so one barrier there both frees s's buffer for stage s + 2
-// and publishes s + 1, whose first fragments are read under the last
-// k-step's products.  The stage sequence runs on over tile ends: the next
-// tile's first two stages load during an epilogue.
-template <class Cfg, typename Epi>
-__device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Epi&& epi) {
-  constexpr int FM = Cfg::FM, FN = Cfg::FN, BK = Cfg::BK;
+// P's and Q's panels of 64 k take turns in a ring of five slots: two are
+// being read, and of the three in flight the older two make up the next stage.
+// A stage's products run in two k-steps of 32 whose fragments are read one
+// k-step ahead; before the second every wave has its last fragments
+// of the stage, so one barrier there both frees the stage's slots (Q's next
+// panel is loaded under the second k-step's products, P's under the next
+// stage's first) and publishes the next stage.  The panel sequence runs on
+// over tile ends: the next tile's first panels load during an epilogue.
+template <class Cfg, typename Pre, typename Epi>
+__device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, Epi&& epi) {
+  constexpr int FM = Cfg::FM, FN = Cfg::FN, BK = Cfg::BK, PANEL = Cfg::PANEL, RING = 5 * PANEL, LOADS = Cfg::LOADS;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / Cfg::WVN, wn = wave % Cfg::WVN;
@@ -157,17 +170,21 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Epi&& epi) 
   const int items = g.mt * g.nt * g.splits;
   if (place >= items) return;
 
-  uint32_t offP[Cfg::PL], offQ[Cfg::QL];
+  // A wave's blocks j and j + 2 differ by whole swizzle periods: two offsets
+  // and a resource each for the even and the odd pair (registers are what
+  // the loop is short of).
+  static_assert(LOADS == 4, "two pairs of blocks");
+  uint32_t offP[2], offQ[2];
 #pragma unroll
-  for (int j = 0; j < Cfg::PL; ++j) offP[j] = bg_lane_off<Cfg::BM, Cfg::PT>(wave * Cfg::PL + j, lane, g.P.ld);
-#pragma unroll
-  for (int j = 0; j < Cfg::QL; ++j) offQ[j] = bg_lane_off<Cfg::BN, Cfg::QT>(wave * Cfg::QL + j, lane, g.Q.ld);
-  char* const ldsP = smem + wave * Cfg::PL * 1024;
-  char* const ldsQ = smem + Cfg::PBYTES + wave * Cfg::QL * 1024;
+  for (int j = 0; j < 2; ++j) {
+    offP[j] = bg_lane_off<Cfg::BM, Cfg::PT>(wave * LOADS + j, lane, g.P.ld);
+    offQ[j] = bg_lane_off<Cfg::BN, Cfg::QT>(wave * LOADS + j, lane, g.Q.ld);
+  }
+  char* const lds0 = smem + wave * LOADS * 1024;
 
-  // the loader's place in the stage sequence
-  int l_item = place, l_buf = 0;
-  int64_t l_left = 0;  // k still to load of the tile
+  // the loader's place in the panel sequence
+  int l_item = place, l_slot = 0;  // l_slot: byte offset of the next panel's slot
+  int64_t l_left = 0;              // k still to load of the tile
   const bf16_t *l_p = nullptr, *l_q = nullptr;
   uint32_t l_np = 0, l_nq = 0;  // bytes of a k-contiguous panel's resource; TR: of a row before the panel
   auto open = [&]() {
@@ -180,30 +197,26 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Epi&& epi) 
     l_np = Cfg::PT ? (uint32_t)(2 * m0) : (uint32_t)((min((int64_t)Cfg::BM, g.M - m0) - 1) * g.P.ld * 2 + 2 * BK);
     l_nq = Cfg::QT ? (uint32_t)(2 * n0) : (uint32_t)((min((int64_t)Cfg::BN, g.N - n0) - 1) * g.Q.ld * 2 + 2 * BK);
   };
-  __amdgpu_buffer_rsrc_t rp, rq;
-  auto stage_open = [&]() {  // resources of the next stage to load
-    uint32_t np = l_np, nq = l_nq;
-    if constexpr (Cfg::PT || Cfg::QT) {
-      const int rows = (int)min(l_left, (int64_t)BK);
-      if constexpr (Cfg::PT) np = (uint32_t)rows * (uint32_t)g.P.ld * 2u - l_np;
-      if constexpr (Cfg::QT) nq = (uint32_t)rows * (uint32_t)g.Q.ld * 2u - l_nq;
-    }
-    rp = uniform_rsrc(l_p, np);
-    rq = uniform_rsrc(l_q, nq);
+  __amdgpu_buffer_rsrc_t rs[2];  // of the panel being issued, from its blocks 0 and 2 of each wave on
+  auto resources = [&](const bf16_t* p, uint32_t bytes, int64_t skip) {  // skip: elements to block 2
+    rs[0] = uniform_rsrc(p, bytes);
+    rs[1] = uniform_rsrc(p + skip, bytes > 2 * skip ? bytes - (uint32_t)(2 * skip) : 0u);
   };
-  auto issue = [&](auto b0c, auto b1c) {
-    constexpr int B0 = decltype(b0c)::value, B1 = decltype(b1c)::value;
-    static_for<B0, B1>([&](auto ic) {
+  constexpr int SKIP_P = Cfg::PT ? 2 * 64 / (Cfg::BM / 8) : 16, SKIP_Q = Cfg::QT ? 2 * 64 / (Cfg::BN / 8) : 16;  // rows
+  auto open_p = [&]() {
+    resources(l_p, Cfg::PT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.P.ld * 2u - l_np : l_np, SKIP_P * g.P.ld);
+  };
+  auto open_q = [&]() {
+    resources(l_q, Cfg::QT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.Q.ld * 2u - l_nq : l_nq, SKIP_Q * g.Q.ld);
+  };
+  auto issue = [&](const uint32_t (&off)[2], auto b0c, auto b1c) {
+    static_for<decltype(b0c)::value, decltype(b1c)::value>([&](auto ic) {
       constexpr int I = decltype(ic)::value;
-      if constexpr (I < Cfg::PL)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rp, (bg_lds_ptr)(ldsP + l_buf + I * 1024), 16, offP[I], 0, 0, 0);
-      else
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (bg_lds_ptr)(ldsQ + l_buf + (I - Cfg::PL) * 1024), 16,
-                                                 offQ[I - Cfg::PL], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[I >> 1], (bg_lds_ptr)(lds0 + l_slot + I * 1024), 16, off[I & 1], 0, 0, 0);
     });
   };
-  auto stage_next = [&]() {  // past the stage just issued
-    l_buf ^= Cfg::STAGE;
+  auto bump = [&]() { l_slot = l_slot + PANEL == RING ? 0 : l_slot + PANEL; };
+  auto stage_next = [&]() {  // past a stage whose P and Q are issued
     l_left -= BK;
     if (l_left > 0) {
       l_p += Cfg::PT ? BK * g.P.ld : BK;
@@ -214,26 +227,27 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Epi&& epi) 
     }
   };
   using C0 = std::integral_constant<int, 0>;
-  using CALL = std::integral_constant<int, Cfg::LOADS>;
+  using CL = std::integral_constant<int, LOADS>;
+  auto panel_p = [&]() { open_p(); issue(offP, C0{}, CL{}); bump(); };
+  auto panel_q = [&]() { open_q(); issue(offQ, C0{}, CL{}); bump(); };
 
   open();
-  stage_open();
-  issue(C0{}, CALL{});
+  panel_p();
+  panel_q();
   stage_next();
   if (l_item < items) {
-    stage_open();
-    issue(C0{}, CALL{});
+    panel_p();
+    panel_q();
     stage_next();
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Cfg::LOADS) : "memory");
-  } else {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (l_item < items) panel_p();
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
 
-  BgPanel<Cfg::BM, FM, Cfg::PT> pp;
-  BgPanel<Cfg::BN, FN, Cfg::QT> pq;
-  pp.init(lds_addr(smem), wm * FM * 32, lane);
-  pq.init(lds_addr(smem) + Cfg::PBYTES, wn * FN * 32, lane);
+  BgPanel<Cfg::BM, Cfg::PT> pp;
+  BgPanel<Cfg::BN, Cfg::QT> pq;
+  pp.init(lds_addr(smem), wm * FM * 16, lane);
+  pq.init(lds_addr(smem) + PANEL, wn * FN * 16, lane);
 
   u32x4 fp[2][FM], fq[2][FN];
   auto read = [&](auto kkc, auto setc, auto ic) {  // fragment IC of k-step KK into set SET: P's, then Q's
@@ -243,62 +257,88 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Epi&& epi) 
     else if constexpr (I < FM + FN)
       pq.template read<KK, I - FM>(fq[SET][I - FM]);
   };
-  static_for<0, FM + FN>([&](auto ic) { read(C0{}, C0{}, ic); });
-  lds_wait0();
-  reg_pin(fp[0]);
-  reg_pin(fq[0]);
 
-  f32x16_t acc[FM][FN];
-  int step = Cfg::STAGE;  // to the other buffer
+  f32x4_t acc[FM][FN];
+  int slot_p = 0, slot_q = PANEL;
+  bool pend = false;  // the P panel after the Q panel issued last is still to be issued
   for (int item = place; item < items; item += G) {
     const BgTile t = bg_tile(g, item);
     const int KS = (int)((min(g.kper, g.K - t.split * g.kper) + BK - 1) / BK);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = f32x16_t{};
+      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{};
+    static_for<0, FM + FN>([&](auto ic) { read(C0{}, C0{}, ic); });
+    lds_wait0();
+    reg_pin(fp[0]);
+    reg_pin(fq[0]);
     for (int s = 0; s < KS; ++s) {
-      const bool more = s + 1 < KS || item + G < items;  // another stage follows
-      static_for<0, 4>([&](auto kkc) {
-        constexpr int KK = decltype(kkc)::value, CB = KK & 1, NB = CB ^ 1, NK = (KK + 1) & 3;
-        bool load = false;
-        if constexpr (KK == 3) {
-          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-          __builtin_amdgcn_s_barrier();
-          pp.shift(step);
-          pq.shift(step);
-          step = -step;
+      const bool more = s + 1 < KS;  // another stage of this tile follows
+      static_for<0, 2>([&](auto kkc) {
+        constexpr int KK = decltype(kkc)::value, CB = KK, NB = KK ^ 1;
+        constexpr int NM = FM * FN, R = FM + FN, H = NM * 3 / 4;
+        bool load;
+        if constexpr (KK == 1) {
           load = l_item < items;
-          if (load) stage_open();
+          // the next stage's P and Q have landed; the P after them may still fly
+          if (load)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+          else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          __builtin_amdgcn_s_barrier();
+          const int np = slot_p + 2 * PANEL >= RING ? slot_p + 2 * PANEL - RING : slot_p + 2 * PANEL;
+          const int nq = slot_q + 2 * PANEL >= RING ? slot_q + 2 * PANEL - RING : slot_q + 2 * PANEL;
+          pp.shift(np - slot_p);
+          pq.shift(nq - slot_q);
+          slot_p = np;
+          slot_q = nq;
+          if (load) open_q();
+          if (!more) pre(t, wm, wn);
+        } else {
+          load = pend;
+          if (load) open_p();
         }
-        constexpr int NM = FM * FN;
         static_for<0, NM>([&](auto xc) {
           constexpr int X = decltype(xc)::value, I = X / FN, J = X % FN;
-          acc[I][J] = mfma32x32x16(as_uint4(fp[CB][I]), as_uint4(fq[CB][J]), acc[I][J]);
-          // the next k-step's fragments over the first half of the products
-          constexpr int R = FM + FN, H = NM / 2 > 0 ? NM / 2 : 1;
+          acc[I][J] = mfma16x16x32(as_uint4(fp[CB][I]), as_uint4(fq[CB][J]), acc[I][J]);
           constexpr int R0 = X < H ? X * R / H : R, R1 = X < H ? (X + 1) * R / H : R;
-          if (KK < 3 || more)
-            static_for<R0, R1>([&](auto ic) {
-              read(std::integral_constant<int, NK>{}, std::integral_constant<int, NB>{}, ic);
-            });
-          if constexpr (KK == 3) {
-            constexpr int L0 = X * Cfg::LOADS / NM, L1 = (X + 1) * Cfg::LOADS / NM;
-            if (load) issue(std::integral_constant<int, L0>{}, std::integral_constant<int, L1>{});
-          }
+          if constexpr (R1 > R0)
+            if (KK == 0 || more)
+              static_for<R0, R1>([&](auto ic) {
+                read(std::integral_constant<int, NB>{}, std::integral_constant<int, NB>{}, ic);
+              });
+          constexpr int L0 = X * LOADS / NM, L1 = (X + 1) * LOADS / NM;
+          if constexpr (L1 > L0)
+            if (load) issue(KK == 1 ? offQ : offP, std::integral_constant<int, L0>{}, std::integral_constant<int, L1>{});
           __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (KK == 3) {
+        if (load) bump();
+        if constexpr (KK == 1) {
           if (load) stage_next();
+          pend = load && l_item < items;
         }
-        lds_wait0();
-        reg_pin(fp[NB]);
-        reg_pin(fq[NB]);
+        if (KK == 0 || more) {
+          lds_wait0();
+          reg_pin(fp[NB]);
+          reg_pin(fq[NB]);
+        }
       });
     }
-    epi(acc, t, wm, wn, lane);
+    epi(acc, t, wm, wn);
   }
 }
+
+// The 4 x 4 outputs of two blocks (i, i + 1) as bf16, eight consecutive m per
+// lane: after the swap of neighbouring 16-lane groups lane l holds m = 16 (i + g % 2)
+// + 8 (g / 2) .. + 7, g = l / 16, of its n.
+__device__ __forceinline__ u32x4 bg_pack8(const f32x4_t& a, const f32x4_t& b) {
+  uint32_t p[4] = {pack_bf2(a[0], a[1]), pack_bf2(a[2], a[3]), pack_bf2(b[0], b[1]), pack_bf2(b[2], b[3])};
+  const auto s0 = __builtin_amdgcn_permlane16_swap(p[0], p[2], false, false);
+  const auto s1 = __builtin_amdgcn_permlane16_swap(p[1], p[3], false, false);
+  return u32x4{s0[0], s1[0], s0[1], s1[1]};
+}
+// The m of bg_pack8's first value relative to block i's first.
+__device__ __forceinline__ int bg_pack8_m(int lane) { return 16 * ((lane >> 4) & 1) + 8 * (lane >> 5); }
 
 }  // namespace
 

@@ -21,57 +21,88 @@ constexpr float NEG_INF = -__builtin_inff();
 
 template <class Cfg>
 struct XentGrid {
-  static constexpr int PER_CU = 2 * 2 * Cfg::STAGE <= 160 * 1024 ? 2 : 1;
+  static constexpr int PER_CU = 2 * Cfg::SMEM <= 160 * 1024 ? 2 : 1;
 };
+#define XENT_KERNEL(C) \
+  __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::NW / 4 * XentGrid<C>::PER_CU))) void
 
 // reference point of a row's exponentials: its maximum, or 0 where that is
 // not finite (exp2(l - 0) then gives 0 for l = -inf, inf for l = inf)
 __device__ __forceinline__ float xent_ref(float m) { return __builtin_isfinite(m) ? m : 0.f; }
 
-// C(m, n) = logit of vocabulary entry m, token n.
-template <class Cfg>
-__global__ __launch_bounds__(Cfg::THREADS) __attribute__((amdgpu_waves_per_eu(Cfg::NW / 4 * XentGrid<Cfg>::PER_CU))) void
-k_xent_lse(BgShape g, XentTok a, float2* part, float* tgt) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) char smem[2 * Cfg::STAGE];
-  bg_run<Cfg>(g, smem, [&](f32x16_t (&acc)[Cfg::FM][Cfg::FN], const BgTile& t, int wm, int wn, int lane) {
-    const int m0 = t.m * Cfg::BM + wm * Cfg::FM * 32, half = lane >> 5;
-    if (m0 + Cfg::FM * 32 > g.M) {  // past the vocabulary: no logit
-#pragma unroll
-      for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (m0 + 32 * i + acc_row(e, lane) >= g.M)
-#pragma unroll
-            for (int j = 0; j < Cfg::FN; ++j) acc[i][j][e] = NEG_INF;
-    }
-#pragma unroll
-    for (int j = 0; j < Cfg::FN; ++j) {
-      const int n = t.n * Cfg::BN + (wn * Cfg::FN + j) * 32 + (lane & 31);
-      float mx = NEG_INF;
-#pragma unroll
-      for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, acc[i][j][e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
-      const float r = -xent_ref(mx) * LOG2E;
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, r));
-      sum += __shfl_xor(sum, 32, WAVE);
-      const int y = n < g.N ? (int)((unsigned)a.y[n] - (unsigned)m0) : -1;
-      if (__any((unsigned)y < (unsigned)(Cfg::FM * 32))) {  // a target's logit is here
-#pragma unroll
-        for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (y == 32 * i + acc_row(e, lane)) tgt[n] = acc[i][j][e];
-      }
-      if (half == 0 && n < g.N) part[(int64_t)(t.m * Cfg::WVM + wm) * g.N + n] = make_float2(mx, sum);
-    }
+// The lane's number as the epilogues take it: opaque, so that what follows from
+// it is computed there and not held in registers through the K loop.
+__device__ __forceinline__ int xent_lane() {
+  int l = threadIdx.x & 63;
+  asm volatile("" : "+v"(l));
+  return l;
+}
+
+// Every accumulator (i, e) of a lane, m = m0 + 16 i + 4 (lane / 16) + e, by
+// compile-time numbers.  (The target and the end of the vocabulary are compared
+// with 16 i + e, the lane's part on their side: those are immediates, the sums would be a
+// register each.)
+template <int FM, typename F>
+__device__ __forceinline__ void xent_each(F&& f) {
+  static_for<0, 4 * FM>([&](auto xc) {
+    constexpr int X = decltype(xc)::value;
+    f(std::integral_constant<int, X / 4>{}, std::integral_constant<int, X % 4>{});
   });
+}
+// f(i, e, it lies at or past m0 + end)
+template <int FM, typename F>
+__device__ __forceinline__ void xent_from(int end, int lane, F&& f) {
+  end -= 4 * (lane >> 4);
+  xent_each<FM>([&](auto i, auto e) { f(i, e, 16 * i + e >= end); });
+}
+
+// C(m, n) = logit of vocabulary entry m, token n.  A wave reduces its 16 FM
+// vocabulary entries of each token in registers (the four lanes that share a
+// token meet by shuffles); the pair goes to part.
+template <class Cfg>
+XENT_KERNEL(Cfg) k_xent_lse(BgShape g, XentTok a, float2* part, float* tgt) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char smem[Cfg::SMEM];
+  constexpr int FM = Cfg::FM, FN = Cfg::FN;
+  bg_run<Cfg>(
+      g, smem, [](const BgTile&, int, int) {},
+      [&](f32x4_t (&acc)[FM][FN], const BgTile& t, int wm, int wn) {
+        const int lane = xent_lane();
+        const int m0 = t.m * Cfg::BM + 16 * wm * FM;
+        int ys[FN];  // used after a j's sums: the loads' time is theirs
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          ys[j] = a.y[min(t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15), g.N - 1)];
+        if (m0 + 16 * FM > g.M) {  // past the vocabulary: no logit
+          xent_from<FM>(g.M - m0, lane, [&](auto i, auto e, bool past) {
+            static_for<0, FN>([&](auto j) { acc[i][j][decltype(e)::value] = past ? NEG_INF : acc[i][j][decltype(e)::value]; });
+          });
+        }
+static_for<0, FN>([&](auto j) {
+          const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
+          float mx = NEG_INF;
+          static_for<0, FM>([&](auto i) {
+            mx = fmaxf(fmaxf(acc[i][j][0], acc[i][j][1]), mx);
+            mx = fmaxf(fmaxf(acc[i][j][2], acc[i][j][3]), mx);
+          });
+          mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
+          const float r = -xent_ref(mx) * LOG2E;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          xent_each<FM>([&](auto i, auto e) { sum[decltype(e)::value] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][decltype(e)::value], LOG2E, r)); });
+          float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          s += __shfl_xor(s, 16, WAVE);
+          s += __shfl_xor(s, 32, WAVE);
+          const int y = (int)((unsigned)ys[j] - (unsigned)m0);
+          if (__any((unsigned)y < 16u * FM)) {  // a target's logit is here
+            float v = 0.f;
+            xent_each<FM>([&](auto i, auto e) { v = y - 4 * (lane >> 4) == 16 * i + e ? acc[i][j][decltype(e)::value] : v; });
+            if (n < g.N && (unsigned)y < 16u * FM && ((y >> 2) & 3) == lane >> 4) tgt[n] = v;
+          }
+          if (lane < 16 && n < g.N) part[(int64_t)(t.m * Cfg::WVM + wm) * g.N + n] = make_float2(mx, s);
+          __builtin_amdgcn_sched_barrier(0);  // one j's values at a time in registers
+        });
+      });
 #endif
 }
 
@@ -105,12 +136,15 @@ __global__ __launch_bounds__(256) void k_xent_join(const float2* __restrict__ pa
   }
 }
 
-// what the backward needs of a token: {lse log2 e, w_t (0 where masked), y, 0};
-// and H with the masked tokens' rows as zeros (their values may be anything,
-// and 0 times an infinity is no zero).
+constexpr int XENT_NEG = 1 << 24;  // above any vocabulary entry
+
+// What the backward needs of a token: tok = {lse log2 e - log2 w, y}, so that
+// exp2(l log2 e - .x) is w exp(l - lse); y is -1 where the token is masked (or
+// w is 0), and where w is negative (.x without w) XENT_NEG is added to it.  And H with the masked tokens' rows as zeros (their values may be
+// anything, and 0 times an infinity is no zero).
 template <typename V>
 __global__ __launch_bounds__(256) void k_xent_prep(const V* __restrict__ H, int T, int cpr, XentTok a,
-                                                   const float* __restrict__ lse, float4* __restrict__ tok,
+                                                   const float* __restrict__ lse, float2* __restrict__ tok,
                                                    V* __restrict__ Hm) {
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int64_t t = i / cpr;
@@ -118,108 +152,132 @@ __global__ __launch_bounds__(256) void k_xent_prep(const V* __restrict__ H, int 
   const int c = (int)(i - t * cpr);
   const int y = a.y[t];
   const float w = y < 0 ? 0.f : a.weight ? a.weight[t] : 1.f;
-  if (c == 0) tok[t] = make_float4(lse[t] * LOG2E, w, __int_as_float(y), 0.f);
+  if (c == 0)  // (a target past any vocabulary stays below XENT_NEG)
+    tok[t] = make_float2(lse[t] * LOG2E - (w > 0.f ? log2f(w) : 0.f),
+                         __int_as_float(w == 0.f ? -1 : min(y, XENT_NEG - 1) + (w > 0.f ? 0 : XENT_NEG)));
   if (Hm) Hm[i] = w != 0.f ? H[i] : V{};
 }
 
 // dl (bf16 [T][ld], columns past the piece zero) of the vocabulary piece that
 // starts at v0.  C(m, n) as in k_xent_lse.
 template <class Cfg>
-__global__ __launch_bounds__(Cfg::THREADS) __attribute__((amdgpu_waves_per_eu(Cfg::NW / 4 * XentGrid<Cfg>::PER_CU))) void
-k_xent_dl(BgShape g, const float4* __restrict__ tok, int v0, bf16_t* __restrict__ dl, int64_t ld) {
+XENT_KERNEL(Cfg) k_xent_dl(BgShape g, XentTok a, const float2* __restrict__ tok, int v0, bf16_t* __restrict__ dl, int64_t ld) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) char smem[2 * Cfg::STAGE];
-  bg_run<Cfg>(g, smem, [&](f32x16_t (&acc)[Cfg::FM][Cfg::FN], const BgTile& t, int wm, int wn, int lane) {
-    const int m0 = t.m * Cfg::BM + wm * Cfg::FM * 32, half = lane >> 5;
+  __shared__ __attribute__((aligned(1024))) char smem[Cfg::SMEM];
+  constexpr int FM = Cfg::FM, FN = Cfg::FN;
+  float2 ks[FN];
+  bg_run<Cfg>(
+      g, smem,
+      [&](const BgTile& t, int wm, int wn) {
+        const int lane = xent_lane();
 #pragma unroll
-    for (int j = 0; j < Cfg::FN; ++j) {
-      const int n = t.n * Cfg::BN + (wn * Cfg::FN + j) * 32 + (lane & 31);
-      const float4 k = n < g.N ? tok[n] : make_float4(0.f, 0.f, __int_as_float(-1), 0.f);
-#pragma unroll
-      for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -k.x));
-      const int y = (int)((unsigned)__float_as_int(k.z) - (unsigned)(v0 + m0));
-      if (__any((unsigned)y < (unsigned)(Cfg::FM * 32))) {
-#pragma unroll
-        for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (y == 32 * i + acc_row(e, lane)) acc[i][j][e] -= 1.f;
-      }
-#pragma unroll
-      for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          acc[i][j][e] = k.y != 0.f && m0 + 32 * i + acc_row(e, lane) < g.M ? acc[i][j][e] * k.y : 0.f;
-      if (n < g.N) {
-        bf16_t* o = dl + (int64_t)n * ld + m0 + 4 * half;
-#pragma unroll
-        for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (m0 + 32 * i + 8 * q < ld)
-              *(uint2*)(o + 32 * i + 8 * q) = make_uint2(pack_bf2(acc[i][j][4 * q], acc[i][j][4 * q + 1]),
-                                                         pack_bf2(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
-      }
-    }
-  });
+        for (int j = 0; j < FN; ++j) {
+          const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
+          ks[j] = tok[min(n, g.N - 1)];
+        }
+      },
+      [&](f32x4_t (&acc)[FM][FN], const BgTile& t, int wm, int wn) {
+        const int lane = xent_lane();
+        const int m0 = t.m * Cfg::BM + 16 * wm * FM;
+        const bool edge = m0 + 16 * FM > g.M;  // past the vocabulary: zeros
+static_for<0, FN>([&](auto j) {
+          const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
+          const float2 k = ks[j];
+          const int yk = __float_as_int(k.y), yt = yk >= XENT_NEG ? yk - XENT_NEG : yk;
+          xent_each<FM>([&](auto i, auto e) {
+            constexpr int E = decltype(e)::value;
+            acc[i][j][E] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][E], LOG2E, -k.x));
+          });
+          if (__any(yk < 0 || yk >= XENT_NEG)) {  // masked tokens; a weight without a logarithm
+            const float f = yk >= XENT_NEG && a.weight && n < g.N ? a.weight[n] : 1.f;
+            xent_each<FM>([&](auto i, auto e) {
+              constexpr int E = decltype(e)::value;
+              acc[i][j][E] = yk < 0 ? 0.f : acc[i][j][E] * f;
+            });
+          }
+          const int y = (int)((unsigned)yt - (unsigned)(v0 + m0));
+          if (__any((unsigned)y < 16u * FM)) {
+            const float w = a.weight && n < g.N ? a.weight[n] : 1.f;
+            xent_each<FM>([&](auto i, auto e) { acc[i][j][decltype(e)::value] -= y - 4 * (lane >> 4) == 16 * i + e ? w : 0.f; });
+          }
+          if (edge) xent_from<FM>(g.M - m0, lane, [&](auto i, auto e, bool past) { acc[i][j][decltype(e)::value] = past ? 0.f : acc[i][j][decltype(e)::value]; });
+          bf16_t* o = dl + (int64_t)n * ld + m0 + bg_pack8_m(lane);
+          static_for<0, FM / 2>([&](auto h) {
+            constexpr int I = 2 * decltype(h)::value;
+            const u32x4 v = bg_pack8(acc[I][j], acc[I + 1][j]);
+            // ld % 64 == 0: a whole pair of blocks or none of it
+            if (n < g.N && m0 + 16 * I < ld) *(u32x4*)(o + 16 * I) = v;
+          });
+          __builtin_amdgcn_sched_barrier(0);  // one j's values at a time in registers
+        });
+      });
 #endif
 }
 
 // out[n][m] (+)= scale C(m, n); rows of masked tokens are zeros (tok given).
 template <class Cfg>
-__global__ __launch_bounds__(Cfg::THREADS) __attribute__((amdgpu_waves_per_eu(Cfg::NW / 4 * XentGrid<Cfg>::PER_CU))) void
-k_xent_out(BgShape g, XentOut o) {
+XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) char smem[2 * Cfg::STAGE];
-  bg_run<Cfg>(g, smem, [&](f32x16_t (&acc)[Cfg::FM][Cfg::FN], const BgTile& t, int wm, int wn, int lane) {
-    const int m0 = t.m * Cfg::BM + wm * Cfg::FM * 32 + 4 * (lane >> 5);
+  __shared__ __attribute__((aligned(1024))) char smem[Cfg::SMEM];
+  constexpr int FM = Cfg::FM, FN = Cfg::FN;
+  int ys[FN];
+  bg_run<Cfg>(
+      g, smem,
+      [&](const BgTile& t, int wm, int wn) {
+        const int lane = xent_lane();
 #pragma unroll
-    for (int j = 0; j < Cfg::FN; ++j) {
-      const int n = t.n * Cfg::BN + (wn * Cfg::FN + j) * 32 + (lane & 31);
-      if (n >= g.N) continue;
-      const bool zero = o.tok && o.tok[n].y == 0.f;
-      const int64_t at = (int64_t)n * o.ld + m0;
-#pragma unroll
-      for (int i = 0; i < Cfg::FM; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (m0 + 32 * i + 8 * q >= g.M) continue;
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = zero ? 0.f : o.scale * acc[i][j][4 * q + e];
-          const int64_t x = at + 32 * i + 8 * q;
-          if (o.f32) {
-            float4* p = (float4*)((float*)o.out + t.split * o.split_stride + x);
-            if (o.add) {
-              const float4 b = *p;
-              v[0] += b.x; v[1] += b.y; v[2] += b.z; v[3] += b.w;
-            }
-            *p = make_float4(v[0], v[1], v[2], v[3]);
-          } else {
-            uint2* p = (uint2*)((bf16_t*)o.out + x);
-            if (o.add) {
-              const uint2 b = *p;
-              v[0] += bf2f(b.x & 0xFFFFu); v[1] += bf2f(b.x >> 16);
-              v[2] += bf2f(b.y & 0xFFFFu); v[3] += bf2f(b.y >> 16);
-            }
-            *p = make_uint2(pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]));
-          }
+        for (int j = 0; j < FN; ++j) {
+          const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
+          ys[j] = o.tok ? __float_as_int(o.tok[min(n, g.N - 1)].y) : 0;
         }
-    }
-  });
+      },
+      [&](f32x4_t (&acc)[FM][FN], const BgTile& t, int wm, int wn) {
+        const int lane = xent_lane();
+        const int m0 = t.m * Cfg::BM + 16 * wm * FM;  // M % 64 == 0: pairs of blocks are whole or not there
+        static_for<0, FN>([&](auto j) {
+          const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
+          const bool zero = ys[j] < 0;
+          static_for<0, FM / 2>([&](auto h) {
+            constexpr int I = 2 * decltype(h)::value;
+            const bool here = n < g.N && m0 + 16 * I < g.M;
+            f32x4_t v[2] = {o.scale * acc[I][j], o.scale * acc[I + 1][j]};
+            if (zero) v[0] = v[1] = f32x4_t{};
+            const int64_t at = (int64_t)n * o.ld + m0 + 16 * I;
+            if (o.f32) {
+              float* p = (float*)o.out + t.split * o.split_stride + at + 4 * (lane >> 4);
+              if (here) {
+                if (o.add) {
+                  v[0] += *(const f32x4_t*)p;
+                  v[1] += *(const f32x4_t*)(p + 16);
+                }
+                *(f32x4_t*)p = v[0];
+                *(f32x4_t*)(p + 16) = v[1];
+              }
+            } else {
+              if (o.add && here) {
+                const bf16_t* p = (const bf16_t*)o.out + at + 4 * (lane >> 4);
+                const uint2 a = *(const uint2*)p, b = *(const uint2*)(p + 16);
+                v[0] += f32x4_t{bf2f(a.x & 0xFFFFu), bf2f(a.x >> 16), bf2f(a.y & 0xFFFFu), bf2f(a.y >> 16)};
+                v[1] += f32x4_t{bf2f(b.x & 0xFFFFu), bf2f(b.x >> 16), bf2f(b.y & 0xFFFFu), bf2f(b.y >> 16)};
+              }
+              const u32x4 w = bg_pack8(v[0], v[1]);
+              if (here) *(u32x4*)((bf16_t*)o.out + at + bg_pack8_m(lane)) = w;
+            }
+          });
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
 #endif
 }
 
 // dH[t] = bf16(scale sum_s part[s][t]) in the order of s, zeros for masked tokens.
 __global__ __launch_bounds__(256) void k_xent_sum(const float4* __restrict__ part, int splits, int64_t n4, int cpr,
-                                                  const float4* __restrict__ tok, float scale,
+                                                  const float2* __restrict__ tok, float scale,
                                                   uint2* __restrict__ dH) {
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= n4) return;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (tok[i / cpr].y != 0.f) {
+  if (__float_as_int(tok[i / cpr].y) >= 0) {
     for (int s = 0; s < splits; ++s) {
       const float4 p = part[s * n4 + i];
       v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
@@ -293,12 +351,12 @@ __global__ void k_xent_check(const int32_t* __restrict__ y, int T, int64_t V, in
   if (t < T && y[t] >= V) *flag = 1;
 }
 
-using Big_cc = BgCfg<2, 4, 4, 2, false, false>;
-using Big_tc = BgCfg<2, 4, 4, 2, true, false>;
-using Big_tt = BgCfg<2, 4, 4, 2, true, true>;
-using Mid_cc = BgCfg<2, 2, 2, 2, false, false>;
-using Mid_tc = BgCfg<2, 2, 2, 2, true, false>;
-using Mid_tt = BgCfg<2, 2, 2, 2, true, true>;
+using Big_cc = BgCfg<2, 4, 8, 4, false, false>;
+using Big_tc = BgCfg<2, 4, 8, 4, true, false>;
+using Big_tt = BgCfg<2, 4, 8, 4, true, true>;
+using Mid_cc = BgCfg<2, 2, 4, 4, false, false>;
+using Mid_tc = BgCfg<2, 2, 4, 4, true, false>;
+using Mid_tt = BgCfg<2, 2, 4, 4, true, true>;
 
 template <class Cfg>
 BgShape shape(const XentGemm& q) {
@@ -355,18 +413,18 @@ hipError_t launch_xent_prep(const void* H, int esize, int T, int d, const XentTo
   const int cpr = d * esize / 16;
   const int64_t n = (int64_t)T * cpr;
   hipLaunchKernelGGL(k_xent_prep<uint4>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, (const uint4*)H, T, cpr, a,
-                     lse, (float4*)tok, (uint4*)Hm);
+                     lse, (float2*)tok, (uint4*)Hm);
   return hipGetLastError();
 }
 
-hipError_t launch_xent_dl(const XentGemm& q, const float* tok, int v0, bf16_t* dl, int64_t ld, hipStream_t s) {
+hipError_t launch_xent_dl(const XentGemm& q, const XentTok& a, const float* tok, int v0, bf16_t* dl, int64_t ld, hipStream_t s) {
   if (!fits(q) || q.K % 64) return hipErrorInvalidValue;
   if (xent_big_tiles(q.M, q.N, 1)) {
     const BgShape g = shape<Big_cc>(q);
-    hipLaunchKernelGGL(k_xent_dl<Big_cc>, grid<Big_cc>(g), dim3(Big_cc::THREADS), 0, s, g, (const float4*)tok, v0, dl, ld);
+    hipLaunchKernelGGL(k_xent_dl<Big_cc>, grid<Big_cc>(g), dim3(Big_cc::THREADS), 0, s, g, a, (const float2*)tok, v0, dl, ld);
   } else {
     const BgShape g = shape<Mid_cc>(q);
-    hipLaunchKernelGGL(k_xent_dl<Mid_cc>, grid<Mid_cc>(g), dim3(Mid_cc::THREADS), 0, s, g, (const float4*)tok, v0, dl, ld);
+    hipLaunchKernelGGL(k_xent_dl<Mid_cc>, grid<Mid_cc>(g), dim3(Mid_cc::THREADS), 0, s, g, a, (const float2*)tok, v0, dl, ld);
   }
   return hipGetLastError();
 }
@@ -394,7 +452,7 @@ hipError_t launch_xent_sum(const float* part, int splits, int T, int d, const fl
                            hipStream_t s) {
   const int64_t n4 = (int64_t)T * d / 4;
   hipLaunchKernelGGL(k_xent_sum, dim3((unsigned)((n4 + 255) / 256)), dim3(256), 0, s, (const float4*)part, splits, n4, d / 4,
-                     (const float4*)tok, scale, (uint2*)dH);
+                     (const float2*)tok, scale, (uint2*)dH);
   return hipGetLastError();
 }
 

@@ -376,21 +376,20 @@ int xent_partials(int64_t V, int64_t T);
 hipError_t launch_xent_lse(const XentGemm& q, const XentTok& a, float* part, float* tgt, hipStream_t s);
 hipError_t launch_xent_join(const float* part, int np, int T, const XentTok& a, const float* tgt, float* loss, float* lse,
                             hipStream_t s);
-// tok [T][4]: lse log2 e, weight (0: masked), target; Hm (may be null): H with
-// the masked rows zero.
+// tok [T][2]: see k_xent_prep; Hm (may be null): H with the masked rows zero.
 hipError_t launch_xent_prep(const void* H, int esize, int T, int d, const XentTok& a, const float* lse, float* tok, void* Hm,
                             hipStream_t s);
 // dl [T][ld] of the vocabulary piece that starts at v0 (q.P its rows, q.M of
 // them); columns q.M .. ld are zeros, ld a multiple of 64.
-hipError_t launch_xent_dl(const XentGemm& q, const float* tok, int v0, bf16_t* dl, int64_t ld, hipStream_t s);
+hipError_t launch_xent_dl(const XentGemm& q, const XentTok& a, const float* tok, int v0, bf16_t* dl, int64_t ld, hipStream_t s);
 // out[n][m] (+)= scale C(m, n), M % 64 == 0; P is [k][m] (what lies past its
 // K-th row reads as zero), Q [n][k] (K padded to 64 with readable columns) or
 // with q_along_rows [k][n].  splits > 1: fp32 out + split * split_stride.  tok
-// given: rows of tokens with weight 0 are zeros.
+// given: rows of masked tokens are zeros.
 struct XentOut {
   void* out; int64_t ld; int f32, add;
   float scale;
-  const float4* tok;
+  const float2* tok;
   int64_t split_stride;
 };
 bool xent_big_tiles(int64_t M, int64_t N, int64_t splits);

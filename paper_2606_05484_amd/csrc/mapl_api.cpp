@@ -1525,7 +1525,7 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
     L.tgt = c.take((size_t)T * 4);
     if (!bf) L.dl = c.take((size_t)T * L.ld * 4);
   } else {
-    L.tok = c.take((size_t)T * 16);
+    L.tok = c.take((size_t)T * 8);
     L.hm = c.take((size_t)T * D.d * es);
     L.dl = c.take((size_t)T * L.ld * es);
     if (bf) {
@@ -1662,11 +1662,11 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
       const int64_t v0 = p * L.piece, n = V - v0 < L.piece ? V - v0 : L.piece;
       const bf16_t* Wp = (const bf16_t*)W + v0 * d;
       LAUNCH("xent_bwd:dl",
-             launch_xent_dl({Wp, d, (const bf16_t*)H, d, (int)n, (int)T, d, 0}, tok, (int)v0, dl, L.ld, s));
+             launch_xent_dl({Wp, d, (const bf16_t*)H, d, (int)n, (int)T, d, 0}, a, tok, (int)v0, dl, L.ld, s));
       if (dH) {
         XentOut o{};
         o.ld = d;
-        o.tok = (const float4*)tok;
+        o.tok = (const float2*)tok;
         if (acc) {
           o.out = acc; o.f32 = 1; o.add = p > 0; o.scale = 1.f; o.split_stride = T * d;
         } else {

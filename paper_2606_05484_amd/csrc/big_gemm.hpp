@@ -46,7 +46,11 @@ struct BgCfg {
   static constexpr int BM = 16 * FM * WVM, BN = 16 * FN * WVN, BK = 64;
   static constexpr int PANEL = BM * BK * 2, SMEM = 5 * PANEL;
   static constexpr int LOADS = PANEL / 1024 / NW;  // 1 KiB direct-to-LDS blocks per wave and panel
-  static_assert(BM == BN, "P and Q panels share a ring of slots");
+  static_assert(BM == BN && LOADS == 4, "P and Q panels share a ring of slots; a wave's blocks go by pairs");
+  // Offsets kept per operand: one for each of a wave's blocks, or (registers
+  // short: the epilogues of exponentials) one for each of a pair, blocks j and
+  // j + 2, which differ by whole swizzle periods, through a resource each.
+  static constexpr int OFFS = PT ? LOADS : 2;
 };
 
 template <int OFF>
@@ -163,6 +167,7 @@ __device__ __forceinline__ BgTile bg_tile(const BgShape& g, int item) {
 template <class Cfg, typename Pre, typename Epi>
 __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, Epi&& epi) {
   constexpr int FM = Cfg::FM, FN = Cfg::FN, BK = Cfg::BK, PANEL = Cfg::PANEL, RING = 5 * PANEL, LOADS = Cfg::LOADS;
+  constexpr int OFFS = Cfg::OFFS;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / Cfg::WVN, wn = wave % Cfg::WVN;
@@ -170,13 +175,9 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
   const int items = g.mt * g.nt * g.splits;
   if (place >= items) return;
 
-  // A wave's blocks j and j + 2 differ by whole swizzle periods: two offsets
-  // and a resource each for the even and the odd pair (registers are what
-  // the loop is short of).
-  static_assert(LOADS == 4, "two pairs of blocks");
-  uint32_t offP[2], offQ[2];
+  uint32_t offP[OFFS], offQ[OFFS];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < OFFS; ++j) {
     offP[j] = bg_lane_off<Cfg::BM, Cfg::PT>(wave * LOADS + j, lane, g.P.ld);
     offQ[j] = bg_lane_off<Cfg::BN, Cfg::QT>(wave * LOADS + j, lane, g.Q.ld);
   }
@@ -197,10 +198,11 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
     l_np = Cfg::PT ? (uint32_t)(2 * m0) : (uint32_t)((min((int64_t)Cfg::BM, g.M - m0) - 1) * g.P.ld * 2 + 2 * BK);
     l_nq = Cfg::QT ? (uint32_t)(2 * n0) : (uint32_t)((min((int64_t)Cfg::BN, g.N - n0) - 1) * g.Q.ld * 2 + 2 * BK);
   };
-  __amdgpu_buffer_rsrc_t rs[2];  // of the panel being issued, from its blocks 0 and 2 of each wave on
+  // of the panel being issued (OFFS == 2: from its blocks 0 and 2 of each wave on)
+  __amdgpu_buffer_rsrc_t rs[LOADS / OFFS];
   auto resources = [&](const bf16_t* p, uint32_t bytes, int64_t skip) {  // skip: elements to block 2
     rs[0] = uniform_rsrc(p, bytes);
-    rs[1] = uniform_rsrc(p + skip, bytes > 2 * skip ? bytes - (uint32_t)(2 * skip) : 0u);
+    if constexpr (OFFS == 2) rs[1] = uniform_rsrc(p + skip, bytes > 2 * skip ? bytes - (uint32_t)(2 * skip) : 0u);
   };
   constexpr int SKIP_P = Cfg::PT ? 2 * 64 / (Cfg::BM / 8) : 16, SKIP_Q = Cfg::QT ? 2 * 64 / (Cfg::BN / 8) : 16;  // rows
   auto open_p = [&]() {
@@ -209,10 +211,11 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
   auto open_q = [&]() {
     resources(l_q, Cfg::QT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.Q.ld * 2u - l_nq : l_nq, SKIP_Q * g.Q.ld);
   };
-  auto issue = [&](const uint32_t (&off)[2], auto b0c, auto b1c) {
+  auto issue = [&](const uint32_t (&off)[OFFS], auto b0c, auto b1c) {
     static_for<decltype(b0c)::value, decltype(b1c)::value>([&](auto ic) {
       constexpr int I = decltype(ic)::value;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[I >> 1], (bg_lds_ptr)(lds0 + l_slot + I * 1024), 16, off[I & 1], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[I / OFFS], (bg_lds_ptr)(lds0 + l_slot + I * 1024), 16, off[I % OFFS], 0, 0,
+                                               0);
     });
   };
   auto bump = [&]() { l_slot = l_slot + PANEL == RING ? 0 : l_slot + PANEL; };

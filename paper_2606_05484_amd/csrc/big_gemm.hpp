@@ -46,11 +46,7 @@ struct BgCfg {
   static constexpr int BM = 16 * FM * WVM, BN = 16 * FN * WVN, BK = 64;
   static constexpr int PANEL = BM * BK * 2, SMEM = 5 * PANEL;
   static constexpr int LOADS = PANEL / 1024 / NW;  // 1 KiB direct-to-LDS blocks per wave and panel
-  static_assert(BM == BN && LOADS == 4, "P and Q panels share a ring of slots; a wave's blocks go by pairs");
-  // Offsets kept per operand: one for each of a wave's blocks, or (registers
-  // short: the epilogues of exponentials) one for each of a pair, blocks j and
-  // j + 2, which differ by whole swizzle periods, through a resource each.
-  static constexpr int OFFS = PT ? LOADS : 2;
+  static_assert(BM == BN, "P and Q panels share a ring of slots");
 };
 
 template <int OFF>
@@ -156,18 +152,19 @@ __device__ __forceinline__ BgTile bg_tile(const BgShape& g, int item) {
 // + 4 (l / 16) + e, n = tile.n BN + 16 (wn FN + j) + l % 16.
 // smem: Cfg::SMEM bytes.
 //
-// P's and Q's panels of 64 k take turns in a ring of five slots: two are
-// being read, and of the three in flight the older two make up the next stage.
-// A stage's products run in two k-steps of 32 whose fragments are read one
-// k-step ahead; before the second every wave has its last fragments
-// of the stage, so one barrier there both frees the stage's slots (Q's next
-// panel is loaded under the second k-step's products, P's under the next
-// stage's first) and publishes the next stage.  The panel sequence runs on
-// over tile ends: the next tile's first panels load during an epilogue.
+// P's and Q's panels of 64 k take turns in a ring of five slots.  A stage's
+// products run in two k-steps of 32 whose fragments are read one k-step
+// ahead; before the second every wave has its last fragments of the
+// stage, so one barrier there both frees the stage's slots and publishes the
+// next stage.  Under the first k-step's products P's panel of the stage after
+// next is loaded, under the second's Q's.  The sequence runs on over tile
+// ends: the next tile's first panels load, and its first fragments are
+// read, before an epilogue.
+// With one wave per SIMD nothing hides a stall, so the products' stream holds no branch: past
+// the last stage the loads go on with empty resources (zeros into free slots).
 template <class Cfg, typename Pre, typename Epi>
 __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, Epi&& epi) {
   constexpr int FM = Cfg::FM, FN = Cfg::FN, BK = Cfg::BK, PANEL = Cfg::PANEL, RING = 5 * PANEL, LOADS = Cfg::LOADS;
-  constexpr int OFFS = Cfg::OFFS;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / Cfg::WVN, wn = wave % Cfg::WVN;
@@ -175,9 +172,9 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
   const int items = g.mt * g.nt * g.splits;
   if (place >= items) return;
 
-  uint32_t offP[OFFS], offQ[OFFS];
+  uint32_t offP[LOADS], offQ[LOADS];
 #pragma unroll
-  for (int j = 0; j < OFFS; ++j) {
+  for (int j = 0; j < LOADS; ++j) {
     offP[j] = bg_lane_off<Cfg::BM, Cfg::PT>(wave * LOADS + j, lane, g.P.ld);
     offQ[j] = bg_lane_off<Cfg::BN, Cfg::QT>(wave * LOADS + j, lane, g.Q.ld);
   }
@@ -185,7 +182,7 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
 
   // the loader's place in the panel sequence
   int l_item = place, l_slot = 0;  // l_slot: byte offset of the next panel's slot
-  int64_t l_left = 0;              // k still to load of the tile
+  int64_t l_left = 0;              // k still to load of the tile; 0: past the last tile
   const bf16_t *l_p = nullptr, *l_q = nullptr;
   uint32_t l_np = 0, l_nq = 0;  // bytes of a k-contiguous panel's resource; TR: of a row before the panel
   auto open = [&]() {
@@ -198,53 +195,47 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
     l_np = Cfg::PT ? (uint32_t)(2 * m0) : (uint32_t)((min((int64_t)Cfg::BM, g.M - m0) - 1) * g.P.ld * 2 + 2 * BK);
     l_nq = Cfg::QT ? (uint32_t)(2 * n0) : (uint32_t)((min((int64_t)Cfg::BN, g.N - n0) - 1) * g.Q.ld * 2 + 2 * BK);
   };
-  // of the panel being issued (OFFS == 2: from its blocks 0 and 2 of each wave on)
-  __amdgpu_buffer_rsrc_t rs[LOADS / OFFS];
-  auto resources = [&](const bf16_t* p, uint32_t bytes, int64_t skip) {  // skip: elements to block 2
-    rs[0] = uniform_rsrc(p, bytes);
-    if constexpr (OFFS == 2) rs[1] = uniform_rsrc(p + skip, bytes > 2 * skip ? bytes - (uint32_t)(2 * skip) : 0u);
-  };
-  constexpr int SKIP_P = Cfg::PT ? 2 * 64 / (Cfg::BM / 8) : 16, SKIP_Q = Cfg::QT ? 2 * 64 / (Cfg::BN / 8) : 16;  // rows
+  __amdgpu_buffer_rsrc_t rs;  // of the panel being issued
   auto open_p = [&]() {
-    resources(l_p, Cfg::PT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.P.ld * 2u - l_np : l_np, SKIP_P * g.P.ld);
+    const uint32_t n = Cfg::PT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.P.ld * 2u - l_np : l_np;
+    rs = uniform_rsrc(l_p, l_left > 0 ? n : 0u);
   };
   auto open_q = [&]() {
-    resources(l_q, Cfg::QT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.Q.ld * 2u - l_nq : l_nq, SKIP_Q * g.Q.ld);
+    const uint32_t n = Cfg::QT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.Q.ld * 2u - l_nq : l_nq;
+    rs = uniform_rsrc(l_q, l_left > 0 ? n : 0u);
   };
-  auto issue = [&](const uint32_t (&off)[OFFS], auto b0c, auto b1c) {
+  auto issue = [&](const uint32_t (&off)[LOADS], auto b0c, auto b1c) {
     static_for<decltype(b0c)::value, decltype(b1c)::value>([&](auto ic) {
       constexpr int I = decltype(ic)::value;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[I / OFFS], (bg_lds_ptr)(lds0 + l_slot + I * 1024), 16, off[I % OFFS], 0, 0,
-                                               0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (bg_lds_ptr)(lds0 + l_slot + I * 1024), 16, off[I], 0, 0, 0);
     });
   };
   auto bump = [&]() { l_slot = l_slot + PANEL == RING ? 0 : l_slot + PANEL; };
   auto stage_next = [&]() {  // past a stage whose P and Q are issued
     l_left -= BK;
-    if (l_left > 0) {
-      l_p += Cfg::PT ? BK * g.P.ld : BK;
-      l_q += Cfg::QT ? BK * g.Q.ld : BK;
-    } else {
+    l_p += Cfg::PT ? BK * g.P.ld : BK;
+    l_q += Cfg::QT ? BK * g.Q.ld : BK;
+    if (l_left <= 0) {
       l_item += G;
+      l_left = 0;
       if (l_item < items) open();
     }
   };
   using C0 = std::integral_constant<int, 0>;
   using CL = std::integral_constant<int, LOADS>;
-  auto panel_p = [&]() { open_p(); issue(offP, C0{}, CL{}); bump(); };
-  auto panel_q = [&]() { open_q(); issue(offQ, C0{}, CL{}); bump(); };
 
   open();
-  panel_p();
-  panel_q();
-  stage_next();
-  if (l_item < items) {
-    panel_p();
-    panel_q();
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    open_p();
+    issue(offP, C0{}, CL{});
+    bump();
+    open_q();
+    issue(offQ, C0{}, CL{});
+    bump();
     stage_next();
-    if (l_item < items) panel_p();
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
   __builtin_amdgcn_s_barrier();
 
   BgPanel<Cfg::BM, Cfg::PT> pp;
@@ -253,41 +244,34 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
   pq.init(lds_addr(smem) + PANEL, wn * FN * 16, lane);
 
   u32x4 fp[2][FM], fq[2][FN];
-  auto read = [&](auto kkc, auto setc, auto ic) {  // fragment IC of k-step KK into set SET: P's, then Q's
-    constexpr int KK = decltype(kkc)::value, SET = decltype(setc)::value, I = decltype(ic)::value;
-    if constexpr (I < FM)
-      pp.template read<KK, I>(fp[SET][I]);
+  auto read = [&](auto kkc, auto ic) {  // fragment IC of k-step KK into its set: Q's, then P's
+    constexpr int KK = decltype(kkc)::value, I = decltype(ic)::value;
+    if constexpr (I < FN)
+      pq.template read<KK, I>(fq[KK][I]);
     else if constexpr (I < FM + FN)
-      pq.template read<KK, I - FM>(fq[SET][I - FM]);
+      pp.template read<KK, I - FN>(fp[KK][I - FN]);
   };
+  static_for<0, FM + FN>([&](auto ic) { read(C0{}, ic); });
+  lds_wait0();
+  reg_pin(fp[0]);
+  reg_pin(fq[0]);
 
   f32x4_t acc[FM][FN];
   int slot_p = 0, slot_q = PANEL;
-  bool pend = false;  // the P panel after the Q panel issued last is still to be issued
   for (int item = place; item < items; item += G) {
     const BgTile t = bg_tile(g, item);
-    const int KS = (int)((min(g.kper, g.K - t.split * g.kper) + BK - 1) / BK);
+    const int KS = __builtin_amdgcn_readfirstlane((int)((min(g.kper, g.K - t.split * g.kper) + BK - 1) / BK));
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{};
-    static_for<0, FM + FN>([&](auto ic) { read(C0{}, C0{}, ic); });
-    lds_wait0();
-    reg_pin(fp[0]);
-    reg_pin(fq[0]);
     for (int s = 0; s < KS; ++s) {
-      const bool more = s + 1 < KS;  // another stage of this tile follows
       static_for<0, 2>([&](auto kkc) {
-        constexpr int KK = decltype(kkc)::value, CB = KK, NB = KK ^ 1;
+        constexpr int KK = decltype(kkc)::value;
         constexpr int NM = FM * FN, R = FM + FN, H = NM * 3 / 4;
-        bool load;
         if constexpr (KK == 1) {
-          load = l_item < items;
           // the next stage's P and Q have landed; the P after them may still fly
-          if (load)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-          else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
           __builtin_amdgcn_s_barrier();
           const int np = slot_p + 2 * PANEL >= RING ? slot_p + 2 * PANEL - RING : slot_p + 2 * PANEL;
           const int nq = slot_q + 2 * PANEL >= RING ? slot_q + 2 * PANEL - RING : slot_q + 2 * PANEL;
@@ -295,40 +279,31 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
           pq.shift(nq - slot_q);
           slot_p = np;
           slot_q = nq;
-          if (load) open_q();
-          if (!more) pre(t, wm, wn);
+          open_q();
+          if (s + 1 == KS) pre(t, wm, wn);
         } else {
-          load = pend;
-          if (load) open_p();
+          open_p();
         }
         static_for<0, NM>([&](auto xc) {
           constexpr int X = decltype(xc)::value, I = X / FN, J = X % FN;
-          acc[I][J] = mfma16x16x32(as_uint4(fp[CB][I]), as_uint4(fq[CB][J]), acc[I][J]);
+          acc[I][J] = mfma16x16x32(as_uint4(fp[KK][I]), as_uint4(fq[KK][J]), acc[I][J]);
           constexpr int R0 = X < H ? X * R / H : R, R1 = X < H ? (X + 1) * R / H : R;
-          if constexpr (R1 > R0)
-            if (KK == 0 || more)
-              static_for<R0, R1>([&](auto ic) {
-                read(std::integral_constant<int, NB>{}, std::integral_constant<int, NB>{}, ic);
-              });
+          static_for<R0, R1>([&](auto ic) { read(std::integral_constant<int, KK ^ 1>{}, ic); });
           constexpr int L0 = X * LOADS / NM, L1 = (X + 1) * LOADS / NM;
-          if constexpr (L1 > L0)
-            if (load) issue(KK == 1 ? offQ : offP, std::integral_constant<int, L0>{}, std::integral_constant<int, L1>{});
+          issue(KK == 1 ? offQ : offP, std::integral_constant<int, L0>{}, std::integral_constant<int, L1>{});
           __builtin_amdgcn_sched_barrier(0);
         });
-        if (load) bump();
-        if constexpr (KK == 1) {
-          if (load) stage_next();
-          pend = load && l_item < items;
-        }
-        if (KK == 0 || more) {
-          lds_wait0();
-          reg_pin(fp[NB]);
-          reg_pin(fq[NB]);
-        }
+        bump();
+        if constexpr (KK == 1) stage_next();
+        lds_wait0();
+        reg_pin(fp[KK ^ 1]);
+        reg_pin(fq[KK ^ 1]);
       });
     }
     epi(acc, t, wm, wn);
   }
+  // nothing may still be written into the LDS of a workgroup that has ended
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 // The 4 x 4 outputs of two blocks (i, i + 1) as bf16, eight consecutive m per

@@ -73,30 +73,34 @@ XENT_KERNEL(Cfg) k_xent_lse(BgShape g, XentTok a, float2* part, float* tgt) {
 #pragma unroll
         for (int j = 0; j < FN; ++j)
           ys[j] = a.y[min(t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15), g.N - 1)];
-        if (m0 + 16 * FM > g.M) {  // past the vocabulary: no logit
-          xent_from<FM>(g.M - m0, lane, [&](auto i, auto e, bool past) {
-            static_for<0, FN>([&](auto j) { acc[i][j][decltype(e)::value] = past ? NEG_INF : acc[i][j][decltype(e)::value]; });
-          });
-        }
-static_for<0, FN>([&](auto j) {
+        const bool edge = m0 + 16 * FM > g.M;  // past the vocabulary: no logit
+        static_for<0, FN>([&](auto j) {
           const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
+          float x[4 * FM];
+          xent_each<FM>([&](auto i, auto e) {
+            float& v = x[4 * i + e];
+            v = acc[i][j][decltype(e)::value];
+            // taken from the accumulators here: two uses of them below would
+            // have the compiler move them between register files in the K loop
+            asm volatile("" : "+v"(v));
+          });
+          if (edge) xent_from<FM>(g.M - m0, lane, [&](auto i, auto e, bool past) { x[4 * i + e] = past ? NEG_INF : x[4 * i + e]; });
           float mx = NEG_INF;
-          static_for<0, FM>([&](auto i) {
-            mx = fmaxf(fmaxf(acc[i][j][0], acc[i][j][1]), mx);
-            mx = fmaxf(fmaxf(acc[i][j][2], acc[i][j][3]), mx);
+          xent_each<FM>([&](auto i, auto e) {
+            if constexpr (decltype(e)::value % 2 == 0) mx = fmaxf(fmaxf(x[4 * i + e], x[4 * i + e + 1]), mx);
           });
           mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
           mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
           const float r = -xent_ref(mx) * LOG2E;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          xent_each<FM>([&](auto i, auto e) { sum[decltype(e)::value] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][decltype(e)::value], LOG2E, r)); });
+          xent_each<FM>([&](auto i, auto e) { sum[e] += __builtin_amdgcn_exp2f(fmaf(x[4 * i + e], LOG2E, r)); });
           float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
           s += __shfl_xor(s, 16, WAVE);
           s += __shfl_xor(s, 32, WAVE);
           const int y = (int)((unsigned)ys[j] - (unsigned)m0);
           if (__any((unsigned)y < 16u * FM)) {  // a target's logit is here
             float v = 0.f;
-            xent_each<FM>([&](auto i, auto e) { v = y - 4 * (lane >> 4) == 16 * i + e ? acc[i][j][decltype(e)::value] : v; });
+            xent_each<FM>([&](auto i, auto e) { v = y - 4 * (lane >> 4) == 16 * i + e ? x[4 * i + e] : v; });
             if (n < g.N && (unsigned)y < 16u * FM && ((y >> 2) & 3) == lane >> 4) tgt[n] = v;
           }
           if (lane < 16 && n < g.N) part[(int64_t)(t.m * Cfg::WVM + wm) * g.N + n] = make_float2(mx, s);
@@ -351,9 +355,9 @@ __global__ void k_xent_check(const int32_t* __restrict__ y, int T, int64_t V, in
   if (t < T && y[t] >= V) *flag = 1;
 }
 
-using Big_cc = BgCfg<2, 4, 8, 4, false, false>;
-using Big_tc = BgCfg<2, 4, 8, 4, true, false>;
-using Big_tt = BgCfg<2, 4, 8, 4, true, true>;
+using Big_cc = BgCfg<2, 2, 8, 8, false, false>;
+using Big_tc = BgCfg<2, 2, 8, 8, true, false>;
+using Big_tt = BgCfg<2, 2, 8, 8, true, true>;
 using Mid_cc = BgCfg<2, 2, 4, 4, false, false>;
 using Mid_tc = BgCfg<2, 2, 4, 4, true, false>;
 using Mid_tt = BgCfg<2, 2, 4, 4, true, true>;

@@ -146,8 +146,8 @@ __device__ __forceinline__ BgTile bg_tile(const BgShape& g, int item) {
 
 // Every tile of this workgroup in turn: item = round gridDim + place, places
 // dealt so that each XCD's workgroups hold consecutive items (gridDim a
-// multiple of 8).  Before a tile's last products pre(tile, wm, wn) may request
-// what its epilogue reads; epi(acc, tile, wm, wn) takes the finished
+// multiple of 8).  Before a tile's products pre(tile, wm, wn) may request what
+// its epilogue reads; epi(acc, tile, wm, wn) takes the finished
 // accumulators: acc[i][j][e] of lane l is C(m, n) at m = tile.m BM + 16 (wm FM + i)
 // + 4 (l / 16) + e, n = tile.n BN + 16 (wn FN + j) + l % 16.
 // smem: Cfg::SMEM bytes.
@@ -195,23 +195,25 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
     l_np = Cfg::PT ? (uint32_t)(2 * m0) : (uint32_t)((min((int64_t)Cfg::BM, g.M - m0) - 1) * g.P.ld * 2 + 2 * BK);
     l_nq = Cfg::QT ? (uint32_t)(2 * n0) : (uint32_t)((min((int64_t)Cfg::BN, g.N - n0) - 1) * g.Q.ld * 2 + 2 * BK);
   };
-  __amdgpu_buffer_rsrc_t rs;  // of the panel being issued
+  __amdgpu_buffer_rsrc_t rsP, rsQ;  // of the panels being issued
   auto open_p = [&]() {
     const uint32_t n = Cfg::PT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.P.ld * 2u - l_np : l_np;
-    rs = uniform_rsrc(l_p, l_left > 0 ? n : 0u);
+    rsP = uniform_rsrc(l_p, l_left > 0 ? n : 0u);
   };
   auto open_q = [&]() {
     const uint32_t n = Cfg::QT ? (uint32_t)min(l_left, (int64_t)BK) * (uint32_t)g.Q.ld * 2u - l_nq : l_nq;
-    rs = uniform_rsrc(l_q, l_left > 0 ? n : 0u);
+    rsQ = uniform_rsrc(l_q, l_left > 0 ? n : 0u);
   };
-  auto issue = [&](const uint32_t (&off)[LOADS], auto b0c, auto b1c) {
+  auto issue = [&](auto qc, auto b0c, auto b1c) {
+    constexpr bool Q = decltype(qc)::value;
     static_for<decltype(b0c)::value, decltype(b1c)::value>([&](auto ic) {
       constexpr int I = decltype(ic)::value;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (bg_lds_ptr)(lds0 + l_slot + I * 1024), 16, off[I], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(Q ? rsQ : rsP, (bg_lds_ptr)(lds0 + l_slot + I * 1024), 16,
+                                               Q ? offQ[I] : offP[I], 0, 0, 0);
     });
   };
   auto bump = [&]() { l_slot = l_slot + PANEL == RING ? 0 : l_slot + PANEL; };
-  auto stage_next = [&]() {  // past a stage whose P and Q are issued
+  auto stage_next = [&]() {  // past a stage whose P and Q resources are made
     l_left -= BK;
     l_p += Cfg::PT ? BK * g.P.ld : BK;
     l_q += Cfg::QT ? BK * g.Q.ld : BK;
@@ -228,13 +230,14 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     open_p();
-    issue(offP, C0{}, CL{});
-    bump();
     open_q();
-    issue(offQ, C0{}, CL{});
+    issue(std::false_type{}, C0{}, CL{});
+    bump();
+    issue(std::true_type{}, C0{}, CL{});
     bump();
     stage_next();
   }
+  open_p();
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
   __builtin_amdgcn_s_barrier();
 
@@ -258,47 +261,59 @@ __device__ __forceinline__ void bg_run(const BgShape& g, char* smem, Pre&& pre, 
 
   f32x4_t acc[FM][FN];
   int slot_p = 0, slot_q = PANEL;
+  // One k-step's products (FIRST: the tile's first, on zeros), the next k-step's
+  // fragments read over their first three quarters, and a panel's loads spread
+  // over all of them.  What the next k-step needs besides is computed between
+  // products too, a few scalar operations at a time.
+  auto kstep = [&](auto kkc, auto firstc) {
+    constexpr int KK = decltype(kkc)::value;
+    constexpr bool FIRST = decltype(firstc)::value;
+    constexpr int NM = FM * FN, R = FM + FN, H = NM * 3 / 4;
+    if constexpr (KK == 1) {
+      // the next stage's P and Q have landed; the P after them may still fly
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+      __builtin_amdgcn_s_barrier();
+    }
+    static_for<0, NM>([&](auto xc) {
+      constexpr int X = decltype(xc)::value, I = X / FN, J = X % FN;
+      acc[I][J] = mfma16x16x32(as_uint4(fp[KK][I]), as_uint4(fq[KK][J]), FIRST ? f32x4_t{} : acc[I][J]);
+      constexpr int R0 = X < H ? X * R / H : R, R1 = X < H ? (X + 1) * R / H : R;
+      static_for<R0, R1>([&](auto ic) { read(std::integral_constant<int, KK ^ 1>{}, ic); });
+      constexpr int L0 = X * LOADS / NM, L1 = (X + 1) * LOADS / NM;
+      issue(std::integral_constant<bool, KK == 1>{}, std::integral_constant<int, L0>{}, std::integral_constant<int, L1>{});
+      if constexpr (KK == 0) {
+        if constexpr (X == NM / 4) open_q();
+        if constexpr (X == H + 1) {  // this stage's fragments are all requested: on to the next one's slots
+          const int np = slot_p + 2 * PANEL >= RING ? slot_p + 2 * PANEL - RING : slot_p + 2 * PANEL;
+          pp.shift(np - slot_p);
+          slot_p = np;
+        }
+        if constexpr (X == H + 2) {
+          const int nq = slot_q + 2 * PANEL >= RING ? slot_q + 2 * PANEL - RING : slot_q + 2 * PANEL;
+          pq.shift(nq - slot_q);
+          slot_q = nq;
+        }
+      } else {
+        if constexpr (X == NM / 4) stage_next();
+        if constexpr (X == NM / 2) open_p();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    bump();
+    lds_wait0();
+    reg_pin(fp[KK ^ 1]);
+    reg_pin(fq[KK ^ 1]);
+  };
+  using C1 = std::integral_constant<int, 1>;
   for (int item = place; item < items; item += G) {
     const BgTile t = bg_tile(g, item);
     const int KS = __builtin_amdgcn_readfirstlane((int)((min(g.kper, g.K - t.split * g.kper) + BK - 1) / BK));
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{};
-    for (int s = 0; s < KS; ++s) {
-      static_for<0, 2>([&](auto kkc) {
-        constexpr int KK = decltype(kkc)::value;
-        constexpr int NM = FM * FN, R = FM + FN, H = NM * 3 / 4;
-        if constexpr (KK == 1) {
-          // the next stage's P and Q have landed; the P after them may still fly
-          asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-          __builtin_amdgcn_s_barrier();
-          const int np = slot_p + 2 * PANEL >= RING ? slot_p + 2 * PANEL - RING : slot_p + 2 * PANEL;
-          const int nq = slot_q + 2 * PANEL >= RING ? slot_q + 2 * PANEL - RING : slot_q + 2 * PANEL;
-          pp.shift(np - slot_p);
-          pq.shift(nq - slot_q);
-          slot_p = np;
-          slot_q = nq;
-          open_q();
-          if (s + 1 == KS) pre(t, wm, wn);
-        } else {
-          open_p();
-        }
-        static_for<0, NM>([&](auto xc) {
-          constexpr int X = decltype(xc)::value, I = X / FN, J = X % FN;
-          acc[I][J] = mfma16x16x32(as_uint4(fp[KK][I]), as_uint4(fq[KK][J]), acc[I][J]);
-          constexpr int R0 = X < H ? X * R / H : R, R1 = X < H ? (X + 1) * R / H : R;
-          static_for<R0, R1>([&](auto ic) { read(std::integral_constant<int, KK ^ 1>{}, ic); });
-          constexpr int L0 = X * LOADS / NM, L1 = (X + 1) * LOADS / NM;
-          issue(KK == 1 ? offQ : offP, std::integral_constant<int, L0>{}, std::integral_constant<int, L1>{});
-          __builtin_amdgcn_sched_barrier(0);
-        });
-        bump();
-        if constexpr (KK == 1) stage_next();
-        lds_wait0();
-        reg_pin(fp[KK ^ 1]);
-        reg_pin(fq[KK ^ 1]);
-      });
+    pre(t, wm, wn);
+    kstep(C0{}, std::true_type{});
+    kstep(C1{}, std::false_type{});
+    for (int s = 1; s < KS; ++s) {
+      kstep(C0{}, std::false_type{});
+      kstep(C1{}, std::false_type{});
     }
     epi(acc, t, wm, wn);
   }

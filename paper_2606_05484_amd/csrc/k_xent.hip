@@ -224,6 +224,7 @@ XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ __attribute__((aligned(1024))) char smem[Cfg::SMEM];
   constexpr int FM = Cfg::FM, FN = Cfg::FN;
+  const float2* const tok = o.tok;
   int ys[FN];
   bg_run<Cfg>(
       g, smem,
@@ -232,7 +233,7 @@ XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
           const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
-          ys[j] = o.tok ? __float_as_int(o.tok[min(n, g.N - 1)].y) : 0;
+          ys[j] = tok ? __float_as_int(tok[min(n, g.N - 1)].y) : 0;
         }
       },
       [&](f32x4_t (&acc)[FM][FN], const BgTile& t, int wm, int wn) {

@@ -110,30 +110,43 @@ XENT_KERNEL(Cfg) k_xent_lse(BgShape g, XentTok a, float2* part, float* tgt) {
 #endif
 }
 
-// lse and loss from `np` partial (maximum, sum) pairs per token; sixteen
-// tokens and sixteen runs of partials per workgroup.
+// lse and loss from `np` partial (maximum, sum) pairs per token: TX tokens and
+// 256 / TX runs of partials per workgroup, four pairs requested at a time.
+// TX = 16 reads whole lines; with few tokens TX = 4 has four times the loads in
+// flight (V = 32000, by events around the launch: 37 tokens 14 -> 7 us, 1021 tokens 10.5 -> 7.0;
+// 2047 tokens 6.6 with TX = 16, 9.7 with 4).
+template <int TX>
 __global__ __launch_bounds__(256) void k_xent_join(const float2* __restrict__ part, int np, int T, XentTok a,
                                                    const float* __restrict__ tgt, float* __restrict__ loss,
                                                    float* __restrict__ lse) {
-  __shared__ float2 sh[16][17];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int t = blockIdx.x * 16 + tx;
+  constexpr int RUNS = 256 / TX, U = 4;
+  __shared__ float2 sh[RUNS][TX + 1];
+  const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
+  const int t = blockIdx.x * TX + tx;
   float m = NEG_INF, s = 0.f;
-  if (t < T)
-    for (int p = ty; p < np; p += 16) {
-      const float2 v = part[(int64_t)p * T + t];
-      const float mn = fmaxf(m, v.x), r = xent_ref(mn);
-      s = s * __builtin_amdgcn_exp2f((xent_ref(m) - r) * LOG2E) + v.y * __builtin_amdgcn_exp2f((xent_ref(v.x) - r) * LOG2E);
-      m = mn;
+  for (int p0 = ty; p0 < np; p0 += RUNS * U) {
+    float2 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = p0 + u * RUNS;
+      v[u] = t < T && p < np ? part[(int64_t)p * T + t] : make_float2(NEG_INF, 0.f);
     }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mn = fmaxf(mn, v[u].x);
+    const float r = xent_ref(mn);
+    s *= __builtin_amdgcn_exp2f((xent_ref(m) - r) * LOG2E);
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += v[u].y * __builtin_amdgcn_exp2f((xent_ref(v[u].x) - r) * LOG2E);
+    m = mn;
+  }
   sh[ty][tx] = make_float2(m, s);
   __syncthreads();
-  if (ty == 0 && t < T) {
-    for (int q = 1; q < 16; ++q) m = fmaxf(m, sh[q][tx].x);
+  if (threadIdx.x < TX && t < T) {
+    for (int q = 1; q < RUNS; ++q) m = fmaxf(m, sh[q][tx].x);
     const float r = xent_ref(m);
     s = 0.f;
-    for (int q = 0; q < 16; ++q)
-      s += sh[q][tx].y * __builtin_amdgcn_exp2f((xent_ref(sh[q][tx].x) - r) * LOG2E);
+    for (int q = 0; q < RUNS; ++q) s += sh[q][tx].y * __builtin_amdgcn_exp2f((xent_ref(sh[q][tx].x) - r) * LOG2E);
     const float L = r + logf(s);
     lse[t] = L;
     loss[t] = a.y[t] < 0 ? 0.f : L - tgt[t];
@@ -146,10 +159,9 @@ constexpr int XENT_NEG = 1 << 24;  // above any vocabulary entry
 // exp2(l log2 e - .x) is w exp(l - lse); y is -1 where the token is masked (or
 // w is 0), and where w is negative (.x without w) XENT_NEG is added to it.  And H with the masked tokens' rows as zeros (their values may be
 // anything, and 0 times an infinity is no zero).
-template <typename V>
-__global__ __launch_bounds__(256) void k_xent_prep(const V* __restrict__ H, int T, int cpr, XentTok a,
+__global__ __launch_bounds__(256) void k_xent_prep(const uint4* __restrict__ H, int T, int cpr, XentTok a,
                                                    const float* __restrict__ lse, float2* __restrict__ tok,
-                                                   V* __restrict__ Hm) {
+                                                   uint4* __restrict__ Hm) {
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int64_t t = i / cpr;
   if (t >= T) return;
@@ -159,7 +171,7 @@ __global__ __launch_bounds__(256) void k_xent_prep(const V* __restrict__ H, int 
   if (c == 0)  // (a target past any vocabulary stays below XENT_NEG)
     tok[t] = make_float2(lse[t] * LOG2E - (w > 0.f ? log2f(w) : 0.f),
                          __int_as_float(w == 0.f ? -1 : min(y, XENT_NEG - 1) + (w > 0.f ? 0 : XENT_NEG)));
-  if (Hm) Hm[i] = w != 0.f ? H[i] : V{};
+  if (Hm) Hm[i] = w != 0.f ? H[i] : make_uint4(0, 0, 0, 0);
 }
 
 // dl (bf16 [T][ld], columns past the piece zero) of the vocabulary piece that
@@ -329,12 +341,17 @@ __global__ __launch_bounds__(256) void k_xent_lse_f32(const float* __restrict__ 
   }
 }
 
+// dl in place; with Hm also the token's row of H, zeros where it is masked.
 __global__ __launch_bounds__(256) void k_xent_dl_f32(float* __restrict__ l, int64_t ld, int n, int v0,
-                                                     const float* __restrict__ lse, XentTok a, float scale) {
+                                                     const float* __restrict__ lse, XentTok a, float scale,
+                                                     const float4* __restrict__ H, float4* __restrict__ Hm, int cpr) {
   const int t = blockIdx.x;
   float* row = l + t * ld;
   const int y = a.y[t];
   const float w = y < 0 ? 0.f : a.weight ? a.weight[t] : 1.f;
+  if (Hm)
+    for (int c = threadIdx.x; c < cpr; c += 256)
+      Hm[(int64_t)t * cpr + c] = w != 0.f ? H[(int64_t)t * cpr + c] : make_float4(0.f, 0.f, 0.f, 0.f);
   const float L = lse[t];
   for (int v = threadIdx.x; v < ld; v += 256) {
     const float p = v < n ? expf(row[v] - L) - (y >= v0 && v == y - v0 ? 1.f : 0.f) : 0.f;
@@ -409,15 +426,18 @@ hipError_t launch_xent_lse(const XentGemm& q, const XentTok& a, float* part, flo
 
 hipError_t launch_xent_join(const float* part, int np, int T, const XentTok& a, const float* tgt, float* loss, float* lse,
                             hipStream_t s) {
-  hipLaunchKernelGGL(k_xent_join, dim3((T + 15) / 16), dim3(256), 0, s, (const float2*)part, np, T, a, tgt, loss, lse);
+  if (T > 1024)
+    hipLaunchKernelGGL(k_xent_join<16>, dim3((T + 15) / 16), dim3(256), 0, s, (const float2*)part, np, T, a, tgt, loss, lse);
+  else
+    hipLaunchKernelGGL(k_xent_join<4>, dim3((T + 3) / 4), dim3(256), 0, s, (const float2*)part, np, T, a, tgt, loss, lse);
   return hipGetLastError();
 }
 
-hipError_t launch_xent_prep(const void* H, int esize, int T, int d, const XentTok& a, const float* lse, float* tok, void* Hm,
+hipError_t launch_xent_prep(const bf16_t* H, int T, int d, const XentTok& a, const float* lse, float* tok, bf16_t* Hm,
                             hipStream_t s) {
-  const int cpr = d * esize / 16;
+  const int cpr = d / 8;
   const int64_t n = (int64_t)T * cpr;
-  hipLaunchKernelGGL(k_xent_prep<uint4>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, (const uint4*)H, T, cpr, a,
+  hipLaunchKernelGGL(k_xent_prep, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, (const uint4*)H, T, cpr, a,
                      lse, (float2*)tok, (uint4*)Hm);
   return hipGetLastError();
 }
@@ -468,8 +488,9 @@ hipError_t launch_xent_lse_f32(const float* l, int64_t ld, int T, int n, int v0,
 }
 
 hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, const float* lse, const XentTok& a, float scale,
-                              hipStream_t s) {
-  hipLaunchKernelGGL(k_xent_dl_f32, dim3(T), dim3(256), 0, s, l, ld, n, v0, lse, a, scale);
+                              const void* H, void* Hm, int d, hipStream_t s) {
+  hipLaunchKernelGGL(k_xent_dl_f32, dim3(T), dim3(256), 0, s, l, ld, n, v0, lse, a, scale, (const float4*)H, (float4*)Hm,
+                     d / 4);
   return hipGetLastError();
 }
 

@@ -377,7 +377,7 @@ hipError_t launch_xent_lse(const XentGemm& q, const XentTok& a, float* part, flo
 hipError_t launch_xent_join(const float* part, int np, int T, const XentTok& a, const float* tgt, float* loss, float* lse,
                             hipStream_t s);
 // tok [T][2]: see k_xent_prep; Hm (may be null): H with the masked rows zero.
-hipError_t launch_xent_prep(const void* H, int esize, int T, int d, const XentTok& a, const float* lse, float* tok, void* Hm,
+hipError_t launch_xent_prep(const bf16_t* H, int T, int d, const XentTok& a, const float* lse, float* tok, bf16_t* Hm,
                             hipStream_t s);
 // dl [T][ld] of the vocabulary piece that starts at v0 (q.P its rows, q.M of
 // them); columns q.M .. ld are zeros, ld a multiple of 64.
@@ -396,11 +396,12 @@ bool xent_big_tiles(int64_t M, int64_t N, int64_t splits);
 hipError_t launch_xent_out(const XentGemm& q, int q_along_rows, const XentOut& o, hipStream_t s);
 hipError_t launch_xent_sum(const float* part, int splits, int T, int d, const float* tok, float scale, bf16_t* dH,
                            hipStream_t s);
-// fp32: n logits per token in rows of ld; dl over them in place (times scale, zeros up to ld).
+// fp32: n logits per token in rows of ld; dl over them in place (times scale, zeros up to ld), and
+// with Hm H with the masked rows zero.
 hipError_t launch_xent_lse_f32(const float* l, int64_t ld, int T, int n, int v0, const XentTok& a, float* part, float* tgt,
                                hipStream_t s);
 hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, const float* lse, const XentTok& a, float scale,
-                              hipStream_t s);
+                              const void* H, void* Hm, int d, hipStream_t s);
 hipError_t launch_xent_zero_rows(float* X, int T, int d, const XentTok& a, hipStream_t s);
 // flag[0] = 1 if any y[t] >= V.
 hipError_t launch_xent_check(const int32_t* y, int T, int64_t V, int* flag, hipStream_t s);

@@ -1525,7 +1525,7 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
     L.tgt = c.take((size_t)T * 4);
     if (!bf) L.dl = c.take((size_t)T * L.ld * 4);
   } else {
-    L.tok = c.take((size_t)T * 8);
+    if (bf) L.tok = c.take((size_t)T * 8);
     L.hm = c.take((size_t)T * D.d * es);
     L.dl = c.take((size_t)T * L.ld * es);
     if (bf) {
@@ -1651,11 +1651,11 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
     return MAPL_OK;
   }
   const XentTok a{targets, weight};
-  float* tok = at<float>(ws, L.tok);
-  void* Hm = at<void>(ws, L.hm);
-  LAUNCH("xent_bwd:prep", launch_xent_prep(H, (int)xe, (int)T, (int)d, a, lse, tok, dW ? Hm : nullptr, s));
 
   if (D.x_dtype == MAPL_BF16) {
+    float* tok = at<float>(ws, L.tok);
+    bf16_t* Hm = at<bf16_t>(ws, L.hm);
+    LAUNCH("xent_bwd:prep", launch_xent_prep((const bf16_t*)H, (int)T, (int)d, a, lse, tok, dW ? Hm : nullptr, s));
     bf16_t* dl = at<bf16_t>(ws, L.dl);
     float* acc = L.acc ? at<float>(ws, L.acc) : nullptr;
     for (int p = 0; p < L.pieces; ++p) {
@@ -1681,7 +1681,7 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
         o.out = (char*)dW + (size_t)v0 * d * esize(D.dw_dtype);
         o.add = accumulate_dW;
         o.scale = scale;
-        LAUNCH("xent_bwd:dW", launch_xent_out({(const bf16_t*)Hm, d, dl, L.ld, (int)d, (int)n, T, 0}, 1, o, s));
+        LAUNCH("xent_bwd:dW", launch_xent_out({Hm, d, dl, L.ld, (int)d, (int)n, T, 0}, 1, o, s));
       }
     }
     if (dH && acc) LAUNCH("xent_bwd:sum", launch_xent_sum(acc, L.splits, (int)T, (int)d, tok, scale, (bf16_t*)dH, s));
@@ -1690,11 +1690,12 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
 
   // ---------------- fp32 path: the vector loads take extents that are
   // multiples of 4; a piece's last one to three entries go on their own
-  float* l = at<float>(ws, L.dl);
+  float *l = at<float>(ws, L.dl), *Hm = at<float>(ws, L.hm);
   for (int p = 0; p < L.pieces; ++p) {
     const int64_t v0 = p * L.piece, n = V - v0 < L.piece ? V - v0 : L.piece;
     LAUNCH("xent_bwd:logits", launch_gemm_f32(xent_logits_f32(D, H, W, v0, n, l, L.ld), s));
-    LAUNCH("xent_bwd:dl", launch_xent_dl_f32(l, L.ld, (int)T, (int)n, (int)v0, lse, a, scale, s));
+    LAUNCH("xent_bwd:dl", launch_xent_dl_f32(l, L.ld, (int)T, (int)n, (int)v0, lse, a, scale, H,
+                                              dW && p == 0 ? Hm : nullptr, (int)d, s));
     for (int64_t u0 = 0; u0 < n; u0 += n & ~(int64_t)3 ? n & ~(int64_t)3 : n) {
       const int64_t m = u0 == 0 && n >= 4 ? n & ~(int64_t)3 : n - u0;
       const float* Wp = (const float*)W + (v0 + u0) * d;

@@ -117,10 +117,25 @@ def _ptr(x):
     return x.data_ptr()
 
 
+_current = None  # torch's current raw stream, a function (torch is imported with the first use)
+
+
+def _current_stream():
+    global _current
+    import torch
+    raw = torch.cuda.current_stream().cuda_stream  # initialises the device
+    C = torch._C
+    if hasattr(C, "_cuda_getCurrentRawStream") and hasattr(C, "_cuda_getDevice"):
+        # without a Stream object: 2 us less a call, a third of what a small call takes on the host
+        _current = lambda: C._cuda_getCurrentRawStream(C._cuda_getDevice())
+    else:
+        _current = lambda: torch.cuda.current_stream().cuda_stream
+    return raw
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current() if _current is not None else _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -230,7 +230,7 @@ static_for<0, FN>([&](auto j) {
 #endif
 }
 
-// out[n][m] (+)= scale C(m, n); rows of masked tokens are zeros (tok given).
+// out[n][m] (+)= scale C(m, n), or scale (C(m, n) + base[n][m]); rows of masked tokens are zeros (tok given).
 template <class Cfg>
 XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -271,6 +271,11 @@ XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
                 *(f32x4_t*)(p + 16) = v[1];
               }
             } else {
+              if (o.base && here) {
+                const float* p = o.base + at + 4 * (lane >> 4);
+                v[0] += o.scale * *(const f32x4_t*)p;
+                v[1] += o.scale * *(const f32x4_t*)(p + 16);
+              }
               if (o.add && here) {
                 const bf16_t* p = (const bf16_t*)o.out + at + 4 * (lane >> 4);
                 const uint2 a = *(const uint2*)p, b = *(const uint2*)(p + 16);

@@ -382,7 +382,7 @@ hipError_t launch_xent_prep(const bf16_t* H, int T, int d, const XentTok& a, con
 // dl [T][ld] of the vocabulary piece that starts at v0 (q.P its rows, q.M of
 // them); columns q.M .. ld are zeros, ld a multiple of 64.
 hipError_t launch_xent_dl(const XentGemm& q, const XentTok& a, const float* tok, int v0, bf16_t* dl, int64_t ld, hipStream_t s);
-// out[n][m] (+)= scale C(m, n), M % 64 == 0; P is [k][m] (what lies past its
+// out[n][m] (+)= scale (C(m, n) + base[n][m]) (base: null, or rows of ld), M % 64 == 0; P is [k][m] (what lies past its
 // K-th row reads as zero), Q [n][k] (K padded to 64 with readable columns) or
 // with q_along_rows [k][n].  splits > 1: fp32 out + split * split_stride.  tok
 // given: rows of masked tokens are zeros.
@@ -391,6 +391,7 @@ struct XentOut {
   float scale;
   const float2* tok;
   int64_t split_stride;
+  const float* base;
 };
 bool xent_big_tiles(int64_t M, int64_t N, int64_t splits);
 hipError_t launch_xent_out(const XentGemm& q, int q_along_rows, const XentOut& o, hipStream_t s);

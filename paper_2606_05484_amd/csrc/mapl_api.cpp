@@ -1667,7 +1667,9 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
         XentOut o{};
         o.ld = d;
         o.tok = (const float2*)tok;
-        if (acc) {
+        if (acc && L.splits == 1 && p == L.pieces - 1) {
+          o.out = dH; o.scale = scale; o.base = acc;
+        } else if (acc) {
           o.out = acc; o.f32 = 1; o.add = p > 0; o.scale = 1.f; o.split_stride = T * d;
         } else {
           o.out = dH; o.scale = scale;
@@ -1684,7 +1686,7 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
         LAUNCH("xent_bwd:dW", launch_xent_out({Hm, d, dl, L.ld, (int)d, (int)n, T, 0}, 1, o, s));
       }
     }
-    if (dH && acc) LAUNCH("xent_bwd:sum", launch_xent_sum(acc, L.splits, (int)T, (int)d, tok, scale, (bf16_t*)dH, s));
+    if (dH && L.splits > 1) LAUNCH("xent_bwd:sum", launch_xent_sum(acc, L.splits, (int)T, (int)d, tok, scale, (bf16_t*)dH, s));
     return MAPL_OK;
   }
 

@@ -230,7 +230,7 @@ static_for<0, FN>([&](auto j) {
 #endif
 }
 
-// out[n][m] (+)= scale C(m, n), or scale (C(m, n) + base[n][m]); rows of masked tokens are zeros (tok given).
+// out[n][m] (+)= scale C(m, n); rows of masked tokens are zeros (tok given).
 template <class Cfg>
 XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -271,11 +271,6 @@ XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
                 *(f32x4_t*)(p + 16) = v[1];
               }
             } else {
-              if (o.base && here) {
-                const float* p = o.base + at + 4 * (lane >> 4);
-                v[0] += o.scale * *(const f32x4_t*)p;
-                v[1] += o.scale * *(const f32x4_t*)(p + 16);
-              }
               if (o.add && here) {
                 const bf16_t* p = (const bf16_t*)o.out + at + 4 * (lane >> 4);
                 const uint2 a = *(const uint2*)p, b = *(const uint2*)(p + 16);
@@ -411,15 +406,27 @@ bool fits(const XentGemm& q) {
 
 }  // namespace
 
-bool xent_big_tiles(int64_t M, int64_t N, int64_t splits) {
-  return (M + 255) / 256 * ((N + 255) / 256) * splits >= 256;
+// 256 x 256 tiles, one workgroup per CU, against 128 x 128 ones, two: the time
+// of a launch is its rounds over the 256 CUs times a round's, and a round of
+// 128-tiles (half the outputs of the other) takes 5/8 of one of 256-tiles, 3/4
+// where K is deep (the same work from twice the LDS and L2 reads, at less
+// power while K is short).  Measured, us, 256 and 128 tiles, d = 1024:
+//   lse  T = 1024: V = 8192 30, 21; V = 9216 29, 34; V = 14336 31, 36;
+//        V = 19200 56, 51; V = 27648 58, 67; T = 8192, V = 24576 338, 380
+//   dW   T = 8192: V = 8192 168, 126; V = 9216 172, 222; V = 19200 366, 391
+//   dl   T = 37, V = 128000 57, 43; dW there 100, 130
+bool xent_big_tiles(int64_t M, int64_t N, int64_t K, int64_t splits) {
+  const int64_t big = (M + 255) / 256 * ((N + 255) / 256) * splits, mid = (M + 127) / 128 * ((N + 127) / 128) * splits;
+  return 8 * ((big + 255) / 256) <= (K > 2048 ? 6 : 5) * ((mid + 511) / 512);
 }
 
-int xent_partials(int64_t V, int64_t T) { return (int)(xent_big_tiles(V, T, 1) ? 2 * ((V + 255) / 256) : 2 * ((V + 127) / 128)); }
+int xent_partials(int64_t V, int64_t T, int64_t d) {
+  return (int)(xent_big_tiles(V, T, d, 1) ? 2 * ((V + 255) / 256) : 2 * ((V + 127) / 128));
+}
 
 hipError_t launch_xent_lse(const XentGemm& q, const XentTok& a, float* part, float* tgt, hipStream_t s) {
   if (!fits(q) || q.K % 64) return hipErrorInvalidValue;
-  if (xent_big_tiles(q.M, q.N, 1)) {
+  if (xent_big_tiles(q.M, q.N, q.K, 1)) {
     const BgShape g = shape<Big_cc>(q);
     hipLaunchKernelGGL(k_xent_lse<Big_cc>, grid<Big_cc>(g), dim3(Big_cc::THREADS), 0, s, g, a, (float2*)part, tgt);
   } else {
@@ -449,7 +456,7 @@ hipError_t launch_xent_prep(const bf16_t* H, int T, int d, const XentTok& a, con
 
 hipError_t launch_xent_dl(const XentGemm& q, const XentTok& a, const float* tok, int v0, bf16_t* dl, int64_t ld, hipStream_t s) {
   if (!fits(q) || q.K % 64) return hipErrorInvalidValue;
-  if (xent_big_tiles(q.M, q.N, 1)) {
+  if (xent_big_tiles(q.M, q.N, q.K, 1)) {
     const BgShape g = shape<Big_cc>(q);
     hipLaunchKernelGGL(k_xent_dl<Big_cc>, grid<Big_cc>(g), dim3(Big_cc::THREADS), 0, s, g, a, (const float2*)tok, v0, dl, ld);
   } else {
@@ -463,7 +470,7 @@ hipError_t launch_xent_out(const XentGemm& q, int q_along_rows, const XentOut& o
   if (!fits(q) || q.M % 64) return hipErrorInvalidValue;
   const int64_t splits = q.kper > 0 ? (q.K + q.kper - 1) / q.kper : 1;
   if (splits > 1 && !o.f32) return hipErrorInvalidValue;
-  const bool big = xent_big_tiles(q.M, q.N, splits);
+  const bool big = xent_big_tiles(q.M, q.N, splits > 1 ? q.kper : q.K, splits);
 #define MAPL_XENT_OUT(C)                                                                          \
   do {                                                                                            \
     const BgShape g = shape<C>(q);                                                                \

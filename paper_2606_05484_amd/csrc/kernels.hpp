@@ -371,8 +371,8 @@ struct XentTok {
   const float* weight;  // [T] or null (ones)
 };
 // M = vocabulary, N = tokens, K = d % 64 == 0, both operands [row][k].
-// part [xent_partials(V, T)][T][2] (maximum, sum of exp), tgt [T] the targets' logits.
-int xent_partials(int64_t V, int64_t T);
+// part [xent_partials(V, T, d)][T][2] (maximum, sum of exp), tgt [T] the targets' logits.
+int xent_partials(int64_t V, int64_t T, int64_t d);
 hipError_t launch_xent_lse(const XentGemm& q, const XentTok& a, float* part, float* tgt, hipStream_t s);
 hipError_t launch_xent_join(const float* part, int np, int T, const XentTok& a, const float* tgt, float* loss, float* lse,
                             hipStream_t s);
@@ -382,7 +382,7 @@ hipError_t launch_xent_prep(const bf16_t* H, int T, int d, const XentTok& a, con
 // dl [T][ld] of the vocabulary piece that starts at v0 (q.P its rows, q.M of
 // them); columns q.M .. ld are zeros, ld a multiple of 64.
 hipError_t launch_xent_dl(const XentGemm& q, const XentTok& a, const float* tok, int v0, bf16_t* dl, int64_t ld, hipStream_t s);
-// out[n][m] (+)= scale (C(m, n) + base[n][m]) (base: null, or rows of ld), M % 64 == 0; P is [k][m] (what lies past its
+// out[n][m] (+)= scale C(m, n), M % 64 == 0; P is [k][m] (what lies past its
 // K-th row reads as zero), Q [n][k] (K padded to 64 with readable columns) or
 // with q_along_rows [k][n].  splits > 1: fp32 out + split * split_stride.  tok
 // given: rows of masked tokens are zeros.
@@ -391,9 +391,8 @@ struct XentOut {
   float scale;
   const float2* tok;
   int64_t split_stride;
-  const float* base;
 };
-bool xent_big_tiles(int64_t M, int64_t N, int64_t splits);
+bool xent_big_tiles(int64_t M, int64_t N, int64_t K, int64_t splits);
 hipError_t launch_xent_out(const XentGemm& q, int q_along_rows, const XentOut& o, hipStream_t s);
 hipError_t launch_xent_sum(const float* part, int splits, int T, int d, const float* tok, float scale, bf16_t* dH,
                            hipStream_t s);

@@ -1497,7 +1497,10 @@ extern "C" int mapl_ckpt_encode_bwd(const mapl_codec_desc* desc, const void* dZ,
 
 // ---------------------------------------------------- vocabulary cross entropy
 namespace {
-// dl of one vocabulary piece (bf16), or its fp32 logits, in the workspace
+// dl of one vocabulary piece (bf16), or its fp32 logits, in the workspace.  A
+// piece more is another pass of dH's fp32 sums (T = 32768, d = 2048, V = 32000,
+// dH and dW: 2 GiB in one piece 2.91 and 3.04 ms, 512 MiB in four 3.25 and 3.22, 128 MiB
+// in 16 4.75 and 6.28).
 constexpr int64_t kXentPieceBytes = (int64_t)512 << 20;
 constexpr int64_t kXentMaxPiece = (int64_t)1 << 21;  // columns (32-bit offsets inside a tile's panel)
 
@@ -1521,7 +1524,7 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
   L.pieces = (int)((D.V + L.piece - 1) / L.piece);
   L.ld = rup(L.piece, 64);
   if (call == MAPL_XENT_FWD) {
-    L.part = c.take((size_t)(bf ? xent_partials(D.V, T) : L.pieces) * T * 8);
+    L.part = c.take((size_t)(bf ? xent_partials(D.V, T, D.d) : L.pieces) * T * 8);
     L.tgt = c.take((size_t)T * 4);
     if (!bf) L.dl = c.take((size_t)T * L.ld * 4);
   } else {
@@ -1529,7 +1532,9 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
     L.hm = c.take((size_t)T * D.d * es);
     L.dl = c.take((size_t)T * L.ld * es);
     if (bf) {
-      // dH has few output tiles: K split over the idle CUs, at least 512 deep
+      // dH has few output tiles: K split over the idle CUs, at least 512 deep (d = 1024, V = 32000, dH and
+      // its sum, us: T = 1021 271 unsplit, 64 + 14 in 16 runs; T = 8192 504 and 388 + 21 in 2; and in a
+      // quarter of the runs 84 + 8 and 508)
       const int64_t tiles = (D.d + 255) / 256 * ((T + 255) / 256);
       int64_t s = tiles < 256 ? 256 / tiles : 1;
       if (s > (L.piece + 511) / 512) s = (L.piece + 511) / 512;
@@ -1610,7 +1615,7 @@ extern "C" int mapl_xent_fwd(const mapl_xent_desc* desc, const void* H, const vo
   int np = L.pieces;
   if (D.x_dtype == MAPL_BF16) {
     XentGemm q{(const bf16_t*)W, d, (const bf16_t*)H, d, (int)V, (int)T, d, 0};
-    np = xent_partials(V, T);
+    np = xent_partials(V, T, d);
     LAUNCH("xent:lse", launch_xent_lse(q, a, part, tgt, s));
   } else {
     float* l = at<float>(ws, L.dl);
@@ -1667,9 +1672,7 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
         XentOut o{};
         o.ld = d;
         o.tok = (const float2*)tok;
-        if (acc && L.splits == 1 && p == L.pieces - 1) {
-          o.out = dH; o.scale = scale; o.base = acc;
-        } else if (acc) {
+        if (acc) {
           o.out = acc; o.f32 = 1; o.add = p > 0; o.scale = 1.f; o.split_stride = T * d;
         } else {
           o.out = dH; o.scale = scale;
@@ -1686,7 +1689,7 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
         LAUNCH("xent_bwd:dW", launch_xent_out({Hm, d, dl, L.ld, (int)d, (int)n, T, 0}, 1, o, s));
       }
     }
-    if (dH && L.splits > 1) LAUNCH("xent_bwd:sum", launch_xent_sum(acc, L.splits, (int)T, (int)d, tok, scale, (bf16_t*)dH, s));
+    if (dH && acc) LAUNCH("xent_bwd:sum", launch_xent_sum(acc, L.splits, (int)T, (int)d, tok, scale, (bf16_t*)dH, s));
     return MAPL_OK;
   }
 

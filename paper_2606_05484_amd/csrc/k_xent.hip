@@ -287,7 +287,9 @@ XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 #endif
 }
 
-// dH[t] = bf16(scale sum_s part[s][t]) in the order of s, zeros for masked tokens.
+// dH[t] = bf16(scale sum_s part[s][t]) in the order of s, zeros for masked tokens; eight
+// terms requested at a time (us, against one: T = 37, d = 2048, 32 runs 7.0, 14.6; T = 100,
+// d = 1024, 64 runs 10.3, 21.5; T = 8192, two runs, 84 MB 20 either way).
 __global__ __launch_bounds__(256) void k_xent_sum(const float4* __restrict__ part, int splits, int64_t n4, int cpr,
                                                   const float2* __restrict__ tok, float scale,
                                                   uint2* __restrict__ dH) {
@@ -295,7 +297,15 @@ __global__ __launch_bounds__(256) void k_xent_sum(const float4* __restrict__ par
   if (i >= n4) return;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   if (__float_as_int(tok[i / cpr].y) >= 0) {
-    for (int s = 0; s < splits; ++s) {
+    int s = 0;
+    for (; s + 8 <= splits; s += 8) {
+      float4 p[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) p[u] = part[(s + u) * n4 + i];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) { v.x += p[u].x; v.y += p[u].y; v.z += p[u].z; v.w += p[u].w; }
+    }
+    for (; s < splits; ++s) {
       const float4 p = part[s * n4 + i];
       v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
     }

@@ -1499,8 +1499,8 @@ extern "C" int mapl_ckpt_encode_bwd(const mapl_codec_desc* desc, const void* dZ,
 namespace {
 // dl of one vocabulary piece (bf16), or its fp32 logits, in the workspace.  A
 // piece more is another pass of dH's fp32 sums (T = 32768, d = 2048, V = 32000,
-// dH and dW: 2 GiB in one piece 2.91 and 3.04 ms, 512 MiB in four 3.25 and 3.22, 128 MiB
-// in 16 4.75 and 6.28).
+// dH and dW: 2 GiB in one piece 2.83 and 2.97 ms, 512 MiB in four 3.31 and 2.89, 128 MiB
+// in 16, whose products have too few tiles for the CUs, 4.78 and 6.22).
 constexpr int64_t kXentPieceBytes = (int64_t)512 << 20;
 constexpr int64_t kXentMaxPiece = (int64_t)1 << 21;  // columns (32-bit offsets inside a tile's panel)
 
@@ -1532,9 +1532,9 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
     L.hm = c.take((size_t)T * D.d * es);
     L.dl = c.take((size_t)T * L.ld * es);
     if (bf) {
-      // dH has few output tiles: K split over the idle CUs, at least 512 deep (d = 1024, V = 32000, dH and
-      // its sum, us: T = 1021 271 unsplit, 64 + 14 in 16 runs; T = 8192 504 and 388 + 21 in 2; and in a
-      // quarter of the runs 84 + 8 and 508)
+      // dH has few output tiles: K split over the idle CUs, at least 512 deep (V = 32000, dH and its sum
+      // in us, unsplit, this, and a quarter of its runs: T = 37, d = 2048 252, 26 + 7, 39 + 7; d = 1024, T = 100 259, 20 + 10,
+      // 25 + 8; T = 1021 271, 64 + 14, 82 + 7; T = 8192 508, 385 + 20, 507)
       const int64_t tiles = (D.d + 255) / 256 * ((T + 255) / 256);
       int64_t s = tiles < 256 ? 256 / tiles : 1;
       if (s > (L.piece + 511) / 512) s = (L.piece + 511) / 512;

@@ -400,8 +400,9 @@ hipError_t launch_xent_sum(const float* part, int splits, int T, int d, const fl
 // with Hm H with the masked rows zero.
 hipError_t launch_xent_lse_f32(const float* l, int64_t ld, int T, int n, int v0, const XentTok& a, float* part, float* tgt,
                                hipStream_t s);
-hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, const float* lse, const XentTok& a, float scale,
-                              const void* H, void* Hm, int d, hipStream_t s);
+// (whole: the piece is all of the vocabulary, normalised by its own sum.)
+hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, bool whole, const float* lse, const XentTok& a,
+                              float scale, const void* H, void* Hm, int d, hipStream_t s);
 hipError_t launch_xent_zero_rows(float* X, int T, int d, const XentTok& a, hipStream_t s);
 // flag[0] = 1 if any y[t] >= V.
 hipError_t launch_xent_check(const int32_t* y, int T, int64_t V, int* flag, hipStream_t s);

@@ -1699,7 +1699,7 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
   for (int p = 0; p < L.pieces; ++p) {
     const int64_t v0 = p * L.piece, n = V - v0 < L.piece ? V - v0 : L.piece;
     LAUNCH("xent_bwd:logits", launch_gemm_f32(xent_logits_f32(D, H, W, v0, n, l, L.ld), s));
-    LAUNCH("xent_bwd:dl", launch_xent_dl_f32(l, L.ld, (int)T, (int)n, (int)v0, lse, a, scale, H,
+    LAUNCH("xent_bwd:dl", launch_xent_dl_f32(l, L.ld, (int)T, (int)n, (int)v0, L.pieces == 1, lse, a, scale, H,
                                               dW && p == 0 ? Hm : nullptr, (int)d, s));
     for (int64_t u0 = 0; u0 < n; u0 += n & ~(int64_t)3 ? n & ~(int64_t)3 : n) {
       const int64_t m = u0 == 0 && n >= 4 ? n & ~(int64_t)3 : n - u0;

@@ -322,33 +322,27 @@ __device__ __forceinline__ void w8_run(const Wgrad8Args& g, char* smem, int spli
   }
   if (s < KS) stage(s, S0{});
 
-  // group 1's sums through LDS, group 0 adds and stores
+  // each group hands the other its sums of one row block through LDS, adds
+  // the other's to its own block and stores it
+  static_assert(FM == 2, "a row block for each group");
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   float* sh = (float*)smem + (wave & 3) * (FM * FN * 16 * 64) + lane;
-  if (grp == 1) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+  for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sh[((i * FN + j) * 16 + e) * 64] = acc[i][j][e];
-  }
+    for (int e = 0; e < 16; ++e) sh[((grp * FN + j) * 16 + e) * 64] = grp ? acc[0][j][e] : acc[1][j][e];
   __syncthreads();
-  if (grp == 1) return;
   const int all = g.d + g.ka;
   float* out = g.part + ((int64_t)split * all + (ANCH ? g.d : 0)) * g.N;
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
+  for (int j = 0; j < FN; ++j) {
+    const int n = n0 + wn * (BN / 2) + j * 32 + (lane & 31);
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int n = n0 + wn * (BN / 2) + j * 32 + (lane & 31);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int m = m0 + wm * 64 + i * 32 + acc_row(e, lane);
-        const float v = acc[i][j][e] + sh[((i * FN + j) * 16 + e) * 64];
-        if (m < rows) out[(int64_t)m * g.N + n] = ANCH ? v : 2.f * v;
-      }
+    for (int e = 0; e < 16; ++e) {
+      const int m = m0 + wm * 64 + grp * 32 + acc_row(e, lane);
+      const float v = (grp ? acc[1][j][e] : acc[0][j][e]) + sh[(((grp ^ 1) * FN + j) * 16 + e) * 64];
+      if (m < rows) out[(int64_t)m * g.N + n] = ANCH ? v : 2.f * v;
     }
   }
 }

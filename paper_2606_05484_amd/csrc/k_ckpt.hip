@@ -327,11 +327,16 @@ __device__ __forceinline__ void w8_run(const Wgrad8Args& g, char* smem, int spli
   static_assert(FM == 2, "a row block for each group");
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  float* sh = (float*)smem + (wave & 3) * (FM * FN * 16 * 64) + lane;
+  f32x4_t* sh = (f32x4_t*)smem + (wave & 3) * (FM * FN * 4 * 64) + lane;
 #pragma unroll
   for (int j = 0; j < FN; ++j)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sh[((grp * FN + j) * 16 + e) * 64] = grp ? acc[0][j][e] : acc[1][j][e];
+    for (int h = 0; h < 4; ++h) {
+      f32x4_t v;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = grp ? acc[0][j][4 * h + u] : acc[1][j][4 * h + u];
+      sh[((grp * FN + j) * 4 + h) * 64] = v;
+    }
   __syncthreads();
   const int all = g.d + g.ka;
   float* out = g.part + ((int64_t)split * all + (ANCH ? g.d : 0)) * g.N;
@@ -339,10 +344,14 @@ __device__ __forceinline__ void w8_run(const Wgrad8Args& g, char* smem, int spli
   for (int j = 0; j < FN; ++j) {
     const int n = n0 + wn * (BN / 2) + j * 32 + (lane & 31);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int m = m0 + wm * 64 + grp * 32 + acc_row(e, lane);
-      const float v = (grp ? acc[1][j][e] : acc[0][j][e]) + sh[(((grp ^ 1) * FN + j) * 16 + e) * 64];
-      if (m < rows) out[(int64_t)m * g.N + n] = ANCH ? v : 2.f * v;
+    for (int h = 0; h < 4; ++h) {
+      const f32x4_t o = sh[(((grp ^ 1) * FN + j) * 4 + h) * 64];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int m = m0 + wm * 64 + grp * 32 + acc_row(4 * h + u, lane);
+        const float v = (grp ? acc[1][j][4 * h + u] : acc[0][j][4 * h + u]) + o[u];
+        if (m < rows) out[(int64_t)m * g.N + n] = ANCH ? v : 2.f * v;
+      }
     }
   }
 }

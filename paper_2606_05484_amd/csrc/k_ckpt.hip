@@ -338,19 +338,20 @@ __device__ __forceinline__ void w8_run(const Wgrad8Args& g, char* smem, int spli
       sh[((grp * FN + j) * 4 + h) * 64] = v;
     }
   __syncthreads();
+  // the rows of the tile in a resource: those past P's end are not stored
   const int all = g.d + g.ka;
-  float* out = g.part + ((int64_t)split * all + (ANCH ? g.d : 0)) * g.N;
+  const float* out = g.part + ((int64_t)split * all + (ANCH ? g.d : 0) + m0) * g.N;
+  const __amdgpu_buffer_rsrc_t ro = uniform_rsrc(out, (uint32_t)(min(W8_BM, rows - m0) * g.N) * 4u);
+  const uint32_t o0 = 4u * (uint32_t)((wm * 64 + grp * 32 + 4 * (lane >> 5)) * g.N + n0 + wn * (BN / 2) + (lane & 31));
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
-    const int n = n0 + wn * (BN / 2) + j * 32 + (lane & 31);
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
       const f32x4_t o = sh[(((grp ^ 1) * FN + j) * 4 + h) * 64];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int m = m0 + wm * 64 + grp * 32 + acc_row(4 * h + u, lane);
         const float v = (grp ? acc[1][j][4 * h + u] : acc[0][j][4 * h + u]) + o[u];
-        if (m < rows) out[(int64_t)m * g.N + n] = ANCH ? v : 2.f * v;
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(ANCH ? v : 2.f * v), ro, o0 + 4u * (uint32_t)((8 * h + u) * g.N), 128 * j, 0);
       }
     }
   }

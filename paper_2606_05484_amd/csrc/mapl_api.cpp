@@ -154,6 +154,24 @@ SplitPlan plan_splits(int64_t T, int Ma, int Mg, int N) {
   return {(int)splits, (int)tps};
 }
 
+// From a checkpoint (the kernel takes 64 tokens in about 1 us), at most
+// sqrt(T / 32) splits: the stages of a split and the partial sums of all,
+// written and read again, cost time as T / S and as S, which are least in sum at a
+// multiple of sqrt(T).  A call in us with the plan above and with this: d = 1024,
+// r = 256, k = 64: T = 300 26.0, 25.4; T = 1021 34.3, 28.6; T = 2048 38.0, 32.7;
+// T = 4096 43.6, 40.3; T = 8192 46.0, 45.8; r = 64, T = 1021 23.5, 22.2; d = 256, r = 64,
+// T = 32768 31.5, 27.3; d = 2048, r = 256, T = 2048 41.7, 42.5.
+SplitPlan plan_splits_ckpt(int64_t T, int Ma, int Mg, int N) {
+  SplitPlan p = plan_splits(T, Ma, Mg, N);
+  int64_t most = 1;
+  while (32 * (most + 1) * (most + 1) <= T) ++most;
+  if (p.splits > most) {
+    p.tps = (int)rup((T + most - 1) / most, 64);
+    p.splits = (int)((T + p.tps - 1) / p.tps);
+  }
+  return p;
+}
+
 constexpr int kStatsInts = 8;  // RVQ decision counters; the rounds' codebook scales follow them
 
 struct Layout {
@@ -223,7 +241,7 @@ Layout layout(const mapl_codec_desc& D, int call, const GradQ* q = nullptr, bool
       case MAPL_CALL_ENCODE_BWD: {
         Lo.w2 = c.take((size_t)d * r * 2);
         const int mg = (amb && k > 0) ? (int)k : 0;
-        Lo.sp = plan_splits(T, (int)d, mg, (int)r);
+        Lo.sp = ck ? plan_splits_ckpt(T, (int)d, mg, (int)r) : plan_splits(T, (int)d, mg, (int)r);
         Lo.part = c.take((size_t)Lo.sp.splits * ((ck ? d : wgrad_row_offset((int)d)) + mg) * r * 4);
         if (mg) {
           Lo.wsum = c.take((size_t)k * r * 4);   // a_s^T dZ

@@ -58,7 +58,9 @@ __device__ __forceinline__ void xent_from(int end, int lane, F&& f) {
 
 // C(m, n) = logit of vocabulary entry m, token n.  A wave reduces its 16 FM
 // vocabulary entries of each token in registers (the four lanes that share a
-// token meet by shuffles); the pair goes to part.
+// token meet by shuffles); the pair goes to part.  Bound by the products
+// (T = 32768, d = 2048, V = 32003 2.97 ms, 1.45 PFLOP/s), with few tokens by W's
+// bytes (T = 37, V = 32000 24 us, 5.5 TB/s).
 template <class Cfg>
 XENT_KERNEL(Cfg) k_xent_lse(BgShape g, XentTok a, float2* part, float* tgt) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -157,8 +159,9 @@ constexpr int XENT_NEG = 1 << 24;  // above any vocabulary entry
 
 // What the backward needs of a token: tok = {lse log2 e - log2 w, y}, so that
 // exp2(l log2 e - .x) is w exp(l - lse); y is -1 where the token is masked (or
-// w is 0), and where w is negative (.x without w) XENT_NEG is added to it.  And H with the masked tokens' rows as zeros (their values may be
-// anything, and 0 times an infinity is no zero).
+// w is 0), and where w is negative (.x without w) XENT_NEG is added to it.  And
+// H with the masked tokens' rows as zeros (their values may be anything, and 0 times an
+// infinity is no zero).  Bound by HBM: [32768, 2048] 268 MB in 45 us, 6 TB/s.
 __global__ __launch_bounds__(256) void k_xent_prep(const uint4* __restrict__ H, int T, int cpr, XentTok a,
                                                    const float* __restrict__ lse, float2* __restrict__ tok,
                                                    uint4* __restrict__ Hm) {
@@ -175,7 +178,9 @@ __global__ __launch_bounds__(256) void k_xent_prep(const uint4* __restrict__ H, 
 }
 
 // dl (bf16 [T][ld], columns past the piece zero) of the vocabulary piece that
-// starts at v0.  C(m, n) as in k_xent_lse.
+// starts at v0.  C(m, n) as in k_xent_lse.  Bound by the products and, after
+// them, by the exponentials (one a logit at a quarter of the vector rate: a quarter of a tile's
+// time at d = 1024).  T = 32768, d = 2048, V = 32000 3.2 ms, 1.35 PFLOP/s.
 template <class Cfg>
 XENT_KERNEL(Cfg) k_xent_dl(BgShape g, XentTok a, const float2* __restrict__ tok, int v0, bf16_t* __restrict__ dl, int64_t ld) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -231,6 +236,8 @@ static_for<0, FN>([&](auto j) {
 }
 
 // out[n][m] (+)= scale C(m, n); rows of masked tokens are zeros (tok given).
+// Bound by the products; T = 32768, d = 2048, V = 32000 in four pieces: dW 2.9 ms, 1.49
+// PFLOP/s, dH, whose fp32 sums are read and written by every piece, 3.2 ms, 1.33.
 template <class Cfg>
 XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 #if defined(__HIP_DEVICE_COMPILE__)

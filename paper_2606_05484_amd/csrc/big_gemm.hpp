@@ -2,14 +2,15 @@
 // on bf16 operands with fp32 accumulation, in tiles of one workgroup per CU.
 // Device code; included by the kernel sources only.
 //
-// What bounds it: with 256 x 256 tiles the matrix units are busy 79-83 % of
-// the time and the clock has fallen to 1.82-1.90 GHz, i.e. the card's power.  Hence
-// the 16 x 16 x 32 instruction (half of the 32 x 32 x 16 one's accumulator
-// traffic per product: 2048 x 32000 x 8192 942 -> 895 us when it came), four waves of
-// 128 x 128 outputs (a fragment from LDS feeds eight products), the XCD-blocked
-// tile order and no operand copied twice.  32000 x 32768 outputs, K = 2048:
-// 1.45 PFLOP/s with the softmax's epilogue, 1.35 with the gradient's (a library's
-// plain product of these sizes reaches 1.37-1.48 on the same card).
+// What bounds it: with 256 x 256 tiles the matrix units are busy 65-75 % of a
+// launch, its epilogues included, and the clock has fallen to 1.82-1.90 GHz,
+// i.e. the card's power.  Hence the 16 x 16 x 32 instruction (half of the 32 x
+// 32 x 16 one's accumulator traffic per product: 2048 x 32000 x 8192 942 -> 895
+// us when it came), four waves of 128 x 128 outputs (a fragment from LDS feeds
+// eight products), the XCD-blocked tile order and no operand copied twice.
+// 32000 x 32768 outputs, K = 2048: 1.45 PFLOP/s with the softmax's epilogue,
+// 1.35 with the gradient's (a library's plain product of these sizes reaches
+// 1.37-1.48 on the same card).
 #pragma once
 #include "common.hpp"
 #include "kernels.hpp"

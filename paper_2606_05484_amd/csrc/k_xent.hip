@@ -30,6 +30,13 @@ struct XentGrid {
 // not finite (exp2(l - 0) then gives 0 for l = -inf, inf for l = inf)
 __device__ __forceinline__ float xent_ref(float m) { return __builtin_isfinite(m) ? m : 0.f; }
 
+// what a sum of exponentials relative to its maximum m counts for relative to
+// r: nothing if there was no logit above -inf (exp(0 - r) may be infinite, and 0
+// times that is no zero)
+__device__ __forceinline__ float xent_rel(float m, float r) {
+  return m == NEG_INF ? 0.f : __builtin_amdgcn_exp2f((xent_ref(m) - r) * LOG2E);
+}
+
 // The lane's number as the epilogues take it: opaque, so that what follows from
 // it is computed there and not held in registers through the K loop.
 __device__ __forceinline__ int xent_lane() {
@@ -137,9 +144,9 @@ __global__ __launch_bounds__(256) void k_xent_join(const float2* __restrict__ pa
 #pragma unroll
     for (int u = 0; u < U; ++u) mn = fmaxf(mn, v[u].x);
     const float r = xent_ref(mn);
-    s *= __builtin_amdgcn_exp2f((xent_ref(m) - r) * LOG2E);
+    s *= xent_rel(m, r);
 #pragma unroll
-    for (int u = 0; u < U; ++u) s += v[u].y * __builtin_amdgcn_exp2f((xent_ref(v[u].x) - r) * LOG2E);
+    for (int u = 0; u < U; ++u) s += v[u].y * xent_rel(v[u].x, r);
     m = mn;
   }
   sh[ty][tx] = make_float2(m, s);
@@ -148,7 +155,7 @@ __global__ __launch_bounds__(256) void k_xent_join(const float2* __restrict__ pa
     for (int q = 1; q < RUNS; ++q) m = fmaxf(m, sh[q][tx].x);
     const float r = xent_ref(m);
     s = 0.f;
-    for (int q = 0; q < RUNS; ++q) s += sh[q][tx].y * __builtin_amdgcn_exp2f((xent_ref(sh[q][tx].x) - r) * LOG2E);
+    for (int q = 0; q < RUNS; ++q) s += sh[q][tx].y * xent_rel(sh[q][tx].x, r);
     const float L = r + logf(s);
     lse[t] = L;
     loss[t] = a.y[t] < 0 ? 0.f : L - tgt[t];

@@ -172,16 +172,16 @@ constexpr int XENT_NEG = 1 << 24;  // above any vocabulary entry
 __global__ __launch_bounds__(256) void k_xent_prep(const uint4* __restrict__ H, int T, int cpr, XentTok a,
                                                    const float* __restrict__ lse, float2* __restrict__ tok,
                                                    uint4* __restrict__ Hm) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int64_t t = i / cpr;
-  if (t >= T) return;
-  const int c = (int)(i - t * cpr);
-  const int y = a.y[t];
-  const float w = y < 0 ? 0.f : a.weight ? a.weight[t] : 1.f;
-  if (c == 0)  // (a target past any vocabulary stays below XENT_NEG)
-    tok[t] = make_float2(lse[t] * LOG2E - (w > 0.f ? log2f(w) : 0.f),
-                         __int_as_float(w == 0.f ? -1 : min(y, XENT_NEG - 1) + (w > 0.f ? 0 : XENT_NEG)));
-  if (Hm) Hm[i] = w != 0.f ? H[i] : make_uint4(0, 0, 0, 0);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)T * cpr; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / cpr;
+    const int c = (int)(i - t * cpr);
+    const int y = a.y[t];
+    const float w = y < 0 ? 0.f : a.weight ? a.weight[t] : 1.f;
+    if (c == 0)  // (a target past any vocabulary stays below XENT_NEG)
+      tok[t] = make_float2(lse[t] * LOG2E - (w > 0.f ? log2f(w) : 0.f),
+                           __int_as_float(w == 0.f ? -1 : min(y, XENT_NEG - 1) + (w > 0.f ? 0 : XENT_NEG)));
+    if (Hm) Hm[i] = w != 0.f ? H[i] : make_uint4(0, 0, 0, 0);
+  }
 }
 
 // dl (bf16 [T][ld], columns past the piece zero) of the vocabulary piece that
@@ -307,24 +307,24 @@ XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 __global__ __launch_bounds__(256) void k_xent_sum(const float4* __restrict__ part, int splits, int64_t n4, int cpr,
                                                   const float2* __restrict__ tok, float scale,
                                                   uint2* __restrict__ dH) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i >= n4) return;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (__float_as_int(tok[i / cpr].y) >= 0) {
-    int s = 0;
-    for (; s + 8 <= splits; s += 8) {
-      float4 p[8];
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (__float_as_int(tok[i / cpr].y) >= 0) {
+      int s = 0;
+      for (; s + 8 <= splits; s += 8) {
+        float4 p[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) p[u] = part[(s + u) * n4 + i];
+        for (int u = 0; u < 8; ++u) p[u] = part[(s + u) * n4 + i];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) { v.x += p[u].x; v.y += p[u].y; v.z += p[u].z; v.w += p[u].w; }
+        for (int u = 0; u < 8; ++u) { v.x += p[u].x; v.y += p[u].y; v.z += p[u].z; v.w += p[u].w; }
+      }
+      for (; s < splits; ++s) {
+        const float4 p = part[s * n4 + i];
+        v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+      }
     }
-    for (; s < splits; ++s) {
-      const float4 p = part[s * n4 + i];
-      v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
-    }
+    dH[i] = make_uint2(pack_bf2(scale * v.x, scale * v.y), pack_bf2(scale * v.z, scale * v.w));
   }
-  dH[i] = make_uint2(pack_bf2(scale * v.x, scale * v.y), pack_bf2(scale * v.z, scale * v.w));
 }
 
 // ------------------------------------------------------------------- fp32
@@ -411,10 +411,10 @@ __global__ __launch_bounds__(256) void k_xent_dl_f32(float* __restrict__ l, int6
 
 // the rows of masked tokens set to zero (0 times an infinite weight row is no zero)
 __global__ __launch_bounds__(256) void k_xent_zero_rows(float4* __restrict__ X, int64_t n4, int cpr, XentTok a) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i >= n4) return;
-  const int64_t t = i / cpr;
-  if (a.y[t] < 0 || (a.weight && a.weight[t] == 0.f)) X[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / cpr;
+    if (a.y[t] < 0 || (a.weight && a.weight[t] == 0.f)) X[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
 }
 
 // bit 0 of flag: a target at or past V
@@ -448,6 +448,11 @@ template <class Cfg>
 dim3 grid(const BgShape& g) {
   const int items = g.mt * g.nt * g.splits, most = 256 * XentGrid<Cfg>::PER_CU;
   return dim3(items < most ? (items + 7) / 8 * 8 : most);
+}
+// workgroups of 256 for n values (a launch holds fewer than 2^32 threads: the rest in turns)
+dim3 blocks_of(int64_t n) {
+  const int64_t b = (n + 255) / 256;
+  return dim3((unsigned)(b < (1 << 23) ? b : 1 << 23));
 }
 bool fits(const XentGemm& q) {
   return q.M > 0 && q.N > 0 && q.K > 0 && q.ldp % 8 == 0 && q.ldq % 8 == 0 && q.ldp <= (1 << 21) && q.ldq <= (1 << 21) &&
@@ -499,7 +504,7 @@ hipError_t launch_xent_prep(const bf16_t* H, int T, int d, const XentTok& a, con
                             hipStream_t s) {
   const int cpr = d / 8;
   const int64_t n = (int64_t)T * cpr;
-  hipLaunchKernelGGL(k_xent_prep, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, (const uint4*)H, T, cpr, a,
+  hipLaunchKernelGGL(k_xent_prep, blocks_of(n), dim3(256), 0, s, (const uint4*)H, T, cpr, a,
                      lse, (float2*)tok, (uint4*)Hm);
   return hipGetLastError();
 }
@@ -538,7 +543,7 @@ hipError_t launch_xent_out(const XentGemm& q, int q_along_rows, const XentOut& o
 hipError_t launch_xent_sum(const float* part, int splits, int T, int d, const float* tok, float scale, bf16_t* dH,
                            hipStream_t s) {
   const int64_t n4 = (int64_t)T * d / 4;
-  hipLaunchKernelGGL(k_xent_sum, dim3((unsigned)((n4 + 255) / 256)), dim3(256), 0, s, (const float4*)part, splits, n4, d / 4,
+  hipLaunchKernelGGL(k_xent_sum, blocks_of(n4), dim3(256), 0, s, (const float4*)part, splits, n4, d / 4,
                      (const float2*)tok, scale, (uint2*)dH);
   return hipGetLastError();
 }
@@ -562,7 +567,7 @@ hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, bool w
 
 hipError_t launch_xent_zero_rows(float* X, int T, int d, const XentTok& a, hipStream_t s) {
   const int64_t n4 = (int64_t)T * d / 4;
-  hipLaunchKernelGGL(k_xent_zero_rows, dim3((unsigned)((n4 + 255) / 256)), dim3(256), 0, s, (float4*)X, n4, d / 4, a);
+  hipLaunchKernelGGL(k_xent_zero_rows, blocks_of(n4), dim3(256), 0, s, (float4*)X, n4, d / 4, a);
   return hipGetLastError();
 }
 

@@ -208,7 +208,7 @@ XENT_KERNEL(Cfg) k_xent_dl(BgShape g, XentTok a, const float2* __restrict__ tok,
         const int lane = xent_lane();
         const int m0 = t.m * Cfg::BM + 16 * wm * FM;
         const bool edge = m0 + 16 * FM > g.M;  // past the vocabulary: zeros
-static_for<0, FN>([&](auto j) {
+        static_for<0, FN>([&](auto j) {
           const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
           const float2 k = ks[j];
           const int yk = __float_as_int(k.y), yt = yk >= XENT_NEG ? yk - XENT_NEG : yk;

@@ -301,29 +301,59 @@ XENT_KERNEL(Cfg) k_xent_out(BgShape g, XentOut o) {
 #endif
 }
 
-// dH[t] = bf16(scale sum_s part[s][t]) in the order of s, zeros for masked tokens; eight
-// terms requested at a time (us, against one: T = 37, d = 2048, 32 runs 7.0, 14.6; T = 100,
+// sum_s part[s][i] in the order of s, eight terms requested at a time
+__device__ __forceinline__ float4 xent_runs_sum(const float4* __restrict__ part, int splits, int64_t n4, int64_t i) {
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  int s = 0;
+  for (; s + 8 <= splits; s += 8) {
+    float4 p[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) p[u] = part[(s + u) * n4 + i];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) { v.x += p[u].x; v.y += p[u].y; v.z += p[u].z; v.w += p[u].w; }
+  }
+  for (; s < splits; ++s) {
+    const float4 p = part[s * n4 + i];
+    v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+  }
+  return v;
+}
+
+// dH[t] = bf16(scale sum_s part[s][t]), zeros for masked tokens (us, against one
+// term requested at a time: T = 37, d = 2048, 32 runs 7.0, 14.6; T = 100,
 // d = 1024, 64 runs 10.3, 21.5; T = 8192, two runs, 84 MB 20 either way).
 __global__ __launch_bounds__(256) void k_xent_sum(const float4* __restrict__ part, int splits, int64_t n4, int cpr,
                                                   const float2* __restrict__ tok, float scale,
                                                   uint2* __restrict__ dH) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (__float_as_int(tok[i / cpr].y) >= 0) {
-      int s = 0;
-      for (; s + 8 <= splits; s += 8) {
-        float4 p[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) p[u] = part[(s + u) * n4 + i];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) { v.x += p[u].x; v.y += p[u].y; v.z += p[u].z; v.w += p[u].w; }
-      }
-      for (; s < splits; ++s) {
-        const float4 p = part[s * n4 + i];
-        v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
-      }
-    }
+    if (__float_as_int(tok[i / cpr].y) >= 0) v = xent_runs_sum(part, splits, n4, i);
     dH[i] = make_uint2(pack_bf2(scale * v.x, scale * v.y), pack_bf2(scale * v.z, scale * v.w));
+  }
+}
+
+// dW (+)= scale sum_s part[s] over the runs of tokens.  Bound by the launch and the
+// partial sums' bytes, at most 64 MB and mostly in the last-level cache.
+__global__ __launch_bounds__(256) void k_xent_sum_dW(const float4* __restrict__ part, int splits, int64_t n4, float scale,
+                                                     void* __restrict__ out, int f32, int add) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
+    float4 v = xent_runs_sum(part, splits, n4, i);
+    v = make_float4(scale * v.x, scale * v.y, scale * v.z, scale * v.w);
+    if (f32) {
+      float4* p = (float4*)out + i;
+      if (add) {
+        const float4 a = *p;
+        v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+      }
+      *p = v;
+    } else {
+      uint2* p = (uint2*)out + i;
+      if (add) {
+        const uint2 a = *p;
+        v.x += bf2f(a.x & 0xFFFFu); v.y += bf2f(a.x >> 16); v.z += bf2f(a.y & 0xFFFFu); v.w += bf2f(a.y >> 16);
+      }
+      *p = make_uint2(pack_bf2(v.x, v.y), pack_bf2(v.z, v.w));
+    }
   }
 }
 
@@ -545,6 +575,13 @@ hipError_t launch_xent_sum(const float* part, int splits, int T, int d, const fl
   const int64_t n4 = (int64_t)T * d / 4;
   hipLaunchKernelGGL(k_xent_sum, blocks_of(n4), dim3(256), 0, s, (const float4*)part, splits, n4, d / 4,
                      (const float2*)tok, scale, (uint2*)dH);
+  return hipGetLastError();
+}
+
+hipError_t launch_xent_sum_dW(const float* part, int splits, int64_t n, float scale, void* out, int f32, int add,
+                              hipStream_t s) {
+  hipLaunchKernelGGL(k_xent_sum_dW, blocks_of(n / 4), dim3(256), 0, s, (const float4*)part, splits, n / 4, scale, out, f32,
+                     add);
   return hipGetLastError();
 }
 

@@ -396,6 +396,9 @@ bool xent_big_tiles(int64_t M, int64_t N, int64_t K, int64_t splits);
 hipError_t launch_xent_out(const XentGemm& q, int q_along_rows, const XentOut& o, hipStream_t s);
 hipError_t launch_xent_sum(const float* part, int splits, int T, int d, const float* tok, float scale, bf16_t* dH,
                            hipStream_t s);
+// out (+)= scale sum_s part[s], n values (a multiple of 4), fp32 or bf16.
+hipError_t launch_xent_sum_dW(const float* part, int splits, int64_t n, float scale, void* out, int f32, int add,
+                              hipStream_t s);
 // fp32: n logits per token in rows of ld; dl over them in place (times scale, zeros up to ld), and
 // with Hm H with the masked rows zero.
 hipError_t launch_xent_lse_f32(const float* l, int64_t ld, int T, int n, int v0, const XentTok& a, float* part, float* tgt,

@@ -15,6 +15,7 @@
 //               Eq. 7 retraction by PolarExpress, batched over projectors.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -1523,10 +1524,36 @@ constexpr int64_t kXentPieceBytes = (int64_t)512 << 20;
 constexpr int64_t kXentMaxPiece = (int64_t)1 << 21;  // columns (32-bit offsets inside a tile's panel)
 
 struct XentLayout {
-  size_t total = 0, flag = 0, part = 0, tgt = 0, tok = 0, hm = 0, dl = 0, acc = 0;
-  int64_t piece = 0, ld = 0, kper = 0;  // vocabulary entries per piece, a row of dl, dH's run of K
-  int pieces = 1, splits = 1;
+  size_t total = 0, flag = 0, part = 0, tgt = 0, tok = 0, hm = 0, dl = 0, acc = 0, accw = 0;
+  int64_t piece = 0, ld = 0;  // vocabulary entries per piece, a row of dl
+  int64_t kper = 0, tper = 0;  // dH's run of K, dW's run of tokens
+  int pieces = 1, splits = 1, tsplits = 1;
 };
+
+// A gradient product with fewer output tiles than CUs splits K into runs of
+// `per`, at least 512 deep and at most `most` of them: returns their number.
+int xent_runs(int64_t M, int64_t N, int64_t K, int64_t most, int64_t* per) {
+  const int64_t tiles = (M + 255) / 256 * ((N + 255) / 256);
+  int64_t s = tiles < 256 ? 256 / tiles : 1;
+  if (s > (K + 511) / 512) s = (K + 511) / 512;
+  if (s > most) s = most;
+  *per = rup((K + s - 1) / s, 64);
+  return (int)((K + *per - 1) / *per);
+}
+
+// Runs of tokens for dW (n vocabulary entries) that pay: a tile's 64 tokens take
+// 0.48 us, a run's sums 8 n d bytes of traffic (about 2 us a million values), the sum's
+// launch 5 us.  The sum of the first two is least at sqrt(3750 T / (n d)) runs; one
+// where even that gains less than it costs.  xent_bwd in us with one run and with
+// these: T = 32768: V = 50, d = 1024 313, 78; V = 256, d = 2048 437, 216; V = 4000,
+// d = 1024 867, 679; V = 32000, d = 256 3014, 2086; T = 8192, d = 1024: V = 256 100,
+// 48; V = 1000 139, 100; T = 2048, V = 256, d = 1024 40, 35.  (Every idle CU a run, without
+// the sums' share: T = 2048, V = 8192, d = 512 89, 104, one run here.)
+int64_t xent_token_runs(int64_t T, int64_t n, int64_t d) {
+  const double work = 0.48 / 64 * (double)T, sums = 2e-6 * (double)(n * d);
+  const int64_t s = (int64_t)std::sqrt(work / sums);
+  return s > 1 && work * (1.0 - 1.0 / (double)s) > 5.0 + sums * (double)s ? s : 1;
+}
 
 XentLayout xent_layout(const mapl_xent_desc& D, int call) {
   XentLayout L;
@@ -1553,12 +1580,11 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
       // dH has few output tiles: K split over the idle CUs, at least 512 deep (V = 32000, dH and its sum
       // in us, unsplit, this, and a quarter of its runs: T = 37, d = 2048 252, 26 + 7, 39 + 7; d = 1024, T = 100 259, 20 + 10,
       // 25 + 8; T = 1021 271, 64 + 14, 82 + 7; T = 8192 508, 385 + 20, 507)
-      const int64_t tiles = (D.d + 255) / 256 * ((T + 255) / 256);
-      int64_t s = tiles < 256 ? 256 / tiles : 1;
-      if (s > (L.piece + 511) / 512) s = (L.piece + 511) / 512;
-      L.kper = rup((L.piece + s - 1) / s, 64);
-      L.splits = (int)((L.piece + L.kper - 1) / L.kper);
+      L.splits = xent_runs(D.d, T, L.piece, 256, &L.kper);
       if (L.splits > 1 || L.pieces > 1) L.acc = c.take((size_t)L.splits * T * D.d * 4);
+      // and dW's tokens, where the vocabulary or a piece of it is short
+      L.tsplits = xent_runs(D.d, L.piece, T, xent_token_runs(T, L.piece, D.d), &L.tper);
+      if (L.tsplits > 1) L.accw = c.take((size_t)L.tsplits * L.piece * D.d * 4);
     }
   }
   L.total = c.off;
@@ -1700,11 +1726,16 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
       if (dW) {
         XentOut o{};
         o.ld = d;
-        o.f32 = D.dw_dtype == MAPL_F32;
-        o.out = (char*)dW + (size_t)v0 * d * esize(D.dw_dtype);
-        o.add = accumulate_dW;
-        o.scale = scale;
-        LAUNCH("xent_bwd:dW", launch_xent_out({Hm, d, dl, L.ld, (int)d, (int)n, T, 0}, 1, o, s));
+        void* out = (char*)dW + (size_t)v0 * d * esize(D.dw_dtype);
+        const int f32 = D.dw_dtype == MAPL_F32;
+        if (L.tsplits > 1) {
+          o.out = at<float>(ws, L.accw); o.f32 = 1; o.scale = 1.f; o.split_stride = n * d;
+        } else {
+          o.out = out; o.f32 = f32; o.add = accumulate_dW; o.scale = scale;
+        }
+        LAUNCH("xent_bwd:dW", launch_xent_out({Hm, d, dl, L.ld, (int)d, (int)n, T, L.tper}, 1, o, s));
+        if (L.tsplits > 1)
+          LAUNCH("xent_bwd:dW_sum", launch_xent_sum_dW(at<float>(ws, L.accw), L.tsplits, n * d, scale, out, f32, accumulate_dW, s));
       }
     }
     if (dH && acc) LAUNCH("xent_bwd:sum", launch_xent_sum(acc, L.splits, (int)T, (int)d, tok, scale, (bf16_t*)dH, s));

@@ -1581,6 +1581,12 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
       // in us, unsplit, this, and a quarter of its runs: T = 37, d = 2048 252, 26 + 7, 39 + 7; d = 1024, T = 100 259, 20 + 10,
       // 25 + 8; T = 1021 271, 64 + 14, 82 + 7; T = 8192 508, 385 + 20, 507)
       L.splits = xent_runs(D.d, T, L.piece, 256, &L.kper);
+      // (a short vocabulary's runs would cost more, by their sum, than they save; by the
+      // model of xent_token_runs.  xent_bwd in us with its runs and with one, d = 1024:
+      // V = 1000: T = 600 37.4, 34.0; T = 1021 43.2, 40.7; T = 8192 99.5, 80.9; V = 4000, T = 8192
+      // 219, 203; the other way V = 1000: T = 500, d = 64 24.7, 26.3; T = 300, d = 256 25.9, 26.5)
+      if (L.pieces == 1 && 0.48 / 64 * (double)D.V * (1.0 - 1.0 / L.splits) < 3.0 + 1e-6 * (double)(T * D.d) * L.splits)
+        L.splits = xent_runs(D.d, T, L.piece, 1, &L.kper);
       if (L.splits > 1 || L.pieces > 1) L.acc = c.take((size_t)L.splits * T * D.d * 4);
       // and dW's tokens, where the vocabulary or a piece of it is short
       L.tsplits = xent_runs(D.d, L.piece, T, xent_token_runs(T, L.piece, D.d), &L.tper);

@@ -30,6 +30,12 @@ struct XentGrid {
 // not finite (exp2(l - 0) then gives 0 for l = -inf, inf for l = inf)
 __device__ __forceinline__ float xent_ref(float m) { return __builtin_isfinite(m) ? m : 0.f; }
 
+// exp(x - ref) is one fma and an exp2, exp2(x log2 e - ref log2 e), whose rounded
+// product ref log2 e is off by up to |ref| 2^-24 (and overflows at the type's end).  Up
+// to this |ref| that is 2^-14 at most, as much as the rounding of a log-sum-exp of that
+// size; past it the difference x - ref is taken first.
+constexpr float XENT_FAR = 1024.f;
+
 // what a sum of exponentials relative to its maximum m counts for relative to
 // r: nothing if there was no logit above -inf (exp(0 - r) may be infinite, and 0
 // times that is no zero)
@@ -100,9 +106,16 @@ XENT_KERNEL(Cfg) k_xent_lse(BgShape g, XentTok a, float2* part, float* tgt) {
           });
           mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
           mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
-          const float r = -xent_ref(mx) * LOG2E;
+          const float ref = xent_ref(mx);
+          const bool far = fabsf(ref) > XENT_FAR;
+          const float r = far ? 0.f : -ref * LOG2E;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          xent_each<FM>([&](auto i, auto e) { sum[e] += __builtin_amdgcn_exp2f(fmaf(x[4 * i + e], LOG2E, r)); });
+          if (__any(far)) {  // (masked runs of the vocabulary; a near token's values are those of the other branch)
+            const float c = far ? ref : 0.f;
+            xent_each<FM>([&](auto i, auto e) { sum[e] += __builtin_amdgcn_exp2f(fmaf(x[4 * i + e] - c, LOG2E, r)); });
+          } else {
+            xent_each<FM>([&](auto i, auto e) { sum[e] += __builtin_amdgcn_exp2f(fmaf(x[4 * i + e], LOG2E, r)); });
+          }
           float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
           s += __shfl_xor(s, 16, WAVE);
           s += __shfl_xor(s, 32, WAVE);

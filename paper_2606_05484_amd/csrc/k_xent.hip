@@ -176,10 +176,12 @@ __global__ __launch_bounds__(256) void k_xent_join(const float2* __restrict__ pa
 }
 
 constexpr int XENT_NEG = 1 << 24;  // above any vocabulary entry
+constexpr int XENT_RAW = 1 << 25;
 
 // What the backward needs of a token: tok = {lse log2 e - log2 w, y}, so that
 // exp2(l log2 e - .x) is w exp(l - lse); y is -1 where the token is masked (or
-// w is 0), and where w is negative (.x without w) XENT_NEG is added to it.  And
+// w is 0), and where w is negative (.x without w) XENT_NEG is added to it.  A
+// token with |lse| past XENT_FAR has .x = lse, and XENT_RAW + XENT_NEG added to y.  And
 // H with the masked tokens' rows as zeros (their values may be anything, and 0 times an
 // infinity is no zero).  Bound by HBM: [32768, 2048] 268 MB in 45 us, 6 TB/s.
 __global__ __launch_bounds__(256) void k_xent_prep(const uint4* __restrict__ H, int T, int cpr, XentTok a,
@@ -190,9 +192,12 @@ __global__ __launch_bounds__(256) void k_xent_prep(const uint4* __restrict__ H, 
     const int c = (int)(i - t * cpr);
     const int y = a.y[t];
     const float w = y < 0 ? 0.f : a.weight ? a.weight[t] : 1.f;
-    if (c == 0)  // (a target past any vocabulary stays below XENT_NEG)
-      tok[t] = make_float2(lse[t] * LOG2E - (w > 0.f ? log2f(w) : 0.f),
-                           __int_as_float(w == 0.f ? -1 : min(y, XENT_NEG - 1) + (w > 0.f ? 0 : XENT_NEG)));
+    if (c == 0) {  // (a target past any vocabulary stays below XENT_NEG)
+      const float L = lse[t];
+      const bool far = fabsf(L) > XENT_FAR;
+      tok[t] = make_float2(far ? L : L * LOG2E - (w > 0.f ? log2f(w) : 0.f),
+                           __int_as_float(w == 0.f ? -1 : min(y, XENT_NEG - 1) + (far ? XENT_RAW + XENT_NEG : w > 0.f ? 0 : XENT_NEG)));
+    }
     if (Hm) Hm[i] = w != 0.f ? H[i] : make_uint4(0, 0, 0, 0);
   }
 }
@@ -224,12 +229,20 @@ XENT_KERNEL(Cfg) k_xent_dl(BgShape g, XentTok a, const float2* __restrict__ tok,
         static_for<0, FN>([&](auto j) {
           const int n = t.n * Cfg::BN + 16 * (wn * FN + j) + (lane & 15);
           const float2 k = ks[j];
-          const int yk = __float_as_int(k.y), yt = yk >= XENT_NEG ? yk - XENT_NEG : yk;
-          xent_each<FM>([&](auto i, auto e) {
-            constexpr int E = decltype(e)::value;
-            acc[i][j][E] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][E], LOG2E, -k.x));
-          });
-          if (__any(yk < 0 || yk >= XENT_NEG)) {  // masked tokens; a weight without a logarithm
+          const int yk = __float_as_int(k.y), yt = yk >= XENT_NEG ? yk & (XENT_NEG - 1) : yk;
+          if (__any(yk >= XENT_RAW)) {
+            const float c = yk >= XENT_RAW ? k.x : 0.f, r = yk >= XENT_RAW ? 0.f : -k.x;
+            xent_each<FM>([&](auto i, auto e) {
+              constexpr int E = decltype(e)::value;
+              acc[i][j][E] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][E] - c, LOG2E, r));
+            });
+          } else {
+            xent_each<FM>([&](auto i, auto e) {
+              constexpr int E = decltype(e)::value;
+              acc[i][j][E] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][E], LOG2E, -k.x));
+            });
+          }
+          if (__any(yk < 0 || yk >= XENT_NEG)) {  // masked tokens; a weight that is not in k.x
             const float f = yk >= XENT_NEG && a.weight && n < g.N ? a.weight[n] : 1.f;
             xent_each<FM>([&](auto i, auto e) {
               constexpr int E = decltype(e)::value;

@@ -310,10 +310,13 @@ size_t mapl_ckpt_encode_bwd_workspace_bytes(const mapl_codec_desc* desc);
  *   the factor all tokens share (1 / tokens for a mean).  accumulate_dW = 0
  *   overwrites dW, 1 adds to it (micro-batches of a step).  dH or dW may be
  *   NULL (a frozen head, or a first-layer probe): its product is left out.
- * fp32, where the vocabulary is one piece of the workspace: the exponentials
- * are divided by their own sum (1 up to rounding) and a target's dl is minus the
- * others' sum, which keeps the digits that exp(l - lse) - 1 loses where the
- * target has nearly all of the probability.
+ *   lse may also be another normaliser, such as that of a larger vocabulary
+ *   which W is a part of (for tokens whose target is in W).
+ * fp32, where the vocabulary is one piece of the workspace and lse is W's own up
+ * to rounding (the logarithm of sum_v exp(l[t,v] - lse[t]) within 2^-24 (256 +
+ * 16 |lse|) of 0): the exponentials are divided by their own sum and a target's dl
+ * is minus the others' sum, which keeps the digits that exp(l - lse) - 1 loses where
+ * the target has nearly all of the probability.
  * bf16: logits, statistics and sums in fp32; dl is rounded to bf16 (before
  * scale, so that the 1 of a target stays exact) for its two products, and dW
  * in bf16 is rounded once per call.  Results are bitwise reproducible.

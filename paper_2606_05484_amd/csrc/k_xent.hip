@@ -421,13 +421,23 @@ __global__ __launch_bounds__(256) void k_xent_lse_f32(const float* __restrict__ 
   }
 }
 
+// Of a token's exponentials exp(l - lse), the target's own and the sum of the
+// others: what all of them are multiplied by and the target's entry of dl.  Where lse
+// is this vocabulary's own log-sum-exp up to rounding (its error as a logarithm within
+// 256 units of 2^-24, and 16 of lse's own), they are divided by their sum and the entry is minus
+// the others' sum, so that a token whose target has nearly all of the probability keeps its
+// gradient's digits: exp(l - lse) - 1 would leave the rounding errors of l and lse there, which are
+// as large (lse from another fp32 product: dH is off by 1.9e-6 of its norm that way at T = 512, d = 256,
+// V = 1000 and by 2.2e-7 this way, at V = 3 by 9.1e-6 and 8.7e-8).  Any other lse counts as it is given.
+__device__ __forceinline__ float2 xent_norm(float others, float own, float lse) {
+  const float s = others + own;
+  if (fabsf(logf(s)) < 0x1p-24f * (256.f + 16.f * fabsf(lse))) return make_float2(1.f / s, -(others * (1.f / s)));
+  return make_float2(1.f, own - 1.f);
+}
+
 // dl in place; with Hm also the token's row of H, zeros where it is masked.
-// WHOLE (the piece is all of the vocabulary): the exponentials are divided by
-// their own sum, and the target's entry is minus the others' sum, so that a token
-// whose target has nearly all of the probability keeps its gradient's digits: exp(l - lse) - 1
-// would leave the rounding errors of l and lse there, which are as large
-// (lse from another fp32 product: dH is off by 1.9e-6 of its norm that way at T = 512, d = 256, V = 1000 and
-// by 2.2e-7 this way, at V = 3 by 9.1e-6 and 8.7e-8; 6.7 and 8.0 us at the former).
+// WHOLE: the piece is all of the vocabulary, normalised as above (T = 512,
+// V = 1000: 8.0 us, without it 6.7).
 template <bool WHOLE>
 __global__ __launch_bounds__(256) void k_xent_dl_f32(float* __restrict__ l, int64_t ld, int n, int v0,
                                                      const float* __restrict__ lse, XentTok a, float scale,
@@ -450,8 +460,9 @@ __global__ __launch_bounds__(256) void k_xent_dl_f32(float* __restrict__ l, int6
       if (v == at) own = p; else others += p;
     }
     others = block_sum(others, sh);
-    inv = 1.f / (others + block_sum(own, sh));
-    ty = -(others * inv);
+    const float2 f = xent_norm(others, block_sum(own, sh), L);
+    inv = f.x;
+    ty = f.y;
   }
   for (int v = threadIdx.x; v < ld; v += 256) {
     float p = 0.f;

@@ -312,11 +312,11 @@ size_t mapl_ckpt_encode_bwd_workspace_bytes(const mapl_codec_desc* desc);
  *   NULL (a frozen head, or a first-layer probe): its product is left out.
  *   lse may also be another normaliser, such as that of a larger vocabulary
  *   which W is a part of (for tokens whose target is in W).
- * fp32, where the vocabulary is one piece of the workspace and lse is W's own up
- * to rounding (the logarithm of sum_v exp(l[t,v] - lse[t]) within 2^-24 (256 +
- * 16 |lse|) of 0): the exponentials are divided by their own sum and a target's dl
- * is minus the others' sum, which keeps the digits that exp(l - lse) - 1 loses where
- * the target has nearly all of the probability.
+ * fp32, where lse is W's own up to rounding (the logarithm of sum_v exp(l[t,v] -
+ * lse[t]) within 2^-24 (256 + 16 |lse|) of 0): the exponentials are divided by their
+ * own sum and a target's dl is minus the others' sum, which keeps the digits that
+ * exp(l - lse) - 1 loses where the target has nearly all of the probability.  (A
+ * vocabulary of several pieces of the workspace has its logits computed twice for it.)
  * bf16: logits, statistics and sums in fp32; dl is rounded to bf16 (before
  * scale, so that the 1 of a target stays exact) for its two products, and dW
  * in bf16 is rounded once per call.  Results are bitwise reproducible.

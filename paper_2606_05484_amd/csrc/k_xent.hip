@@ -435,13 +435,35 @@ __device__ __forceinline__ float2 xent_norm(float others, float own, float lse) 
   return make_float2(1.f, own - 1.f);
 }
 
+// sums[t] (+)= {the others' exponentials, the target's own} of the piece at v0, for
+// xent_norm over a vocabulary of several pieces.
+__global__ __launch_bounds__(256) void k_xent_sums_f32(const float* __restrict__ l, int64_t ld, int n, int v0,
+                                                       const float* __restrict__ lse, XentTok a, float2* __restrict__ sums) {
+  __shared__ float sh[4];
+  const int t = blockIdx.x;
+  const float* row = l + t * ld;
+  const int y = a.y[t], at = y >= v0 && y - v0 < n ? y - v0 : -1;
+  const float L = lse[t];
+  float others = 0.f, own = 0.f;
+  for (int v = threadIdx.x; v < n; v += 256) {
+    const float p = expf(row[v] - L);
+    if (v == at) own = p; else others += p;
+  }
+  others = block_sum(others, sh);
+  own = block_sum(own, sh);
+  if (threadIdx.x == 0) {
+    const float2 before = v0 > 0 ? sums[t] : make_float2(0.f, 0.f);
+    sums[t] = make_float2(before.x + others, before.y + own);
+  }
+}
+
 // dl in place; with Hm also the token's row of H, zeros where it is masked.
-// WHOLE: the piece is all of the vocabulary, normalised as above (T = 512,
-// V = 1000: 8.0 us, without it 6.7).
+// WHOLE: the piece is all of the vocabulary, whose sums are taken here (T = 512,
+// V = 1000: 8.0 us, without them 6.7); else they are in `sums`.
 template <bool WHOLE>
 __global__ __launch_bounds__(256) void k_xent_dl_f32(float* __restrict__ l, int64_t ld, int n, int v0,
-                                                     const float* __restrict__ lse, XentTok a, float scale,
-                                                     const float4* __restrict__ H, float4* __restrict__ Hm, int cpr) {
+                                                     const float* __restrict__ lse, const float2* __restrict__ sums, XentTok a,
+                                                     float scale, const float4* __restrict__ H, float4* __restrict__ Hm, int cpr) {
   __shared__ float sh[4];
   const int t = blockIdx.x;
   float* row = l + t * ld;
@@ -451,7 +473,7 @@ __global__ __launch_bounds__(256) void k_xent_dl_f32(float* __restrict__ l, int6
     for (int c = threadIdx.x; c < cpr; c += 256)
       Hm[(int64_t)t * cpr + c] = w != 0.f ? H[(int64_t)t * cpr + c] : make_float4(0.f, 0.f, 0.f, 0.f);
   const float L = lse[t];
-  float inv = 1.f, ty = 0.f;  // what the exponentials are multiplied by, the target's entry
+  float2 f;  // what the exponentials are multiplied by, the target's entry
   if constexpr (WHOLE) {
     float others = 0.f, own = 0.f;
     for (int v = threadIdx.x; v < n; v += 256) {
@@ -460,18 +482,13 @@ __global__ __launch_bounds__(256) void k_xent_dl_f32(float* __restrict__ l, int6
       if (v == at) own = p; else others += p;
     }
     others = block_sum(others, sh);
-    const float2 f = xent_norm(others, block_sum(own, sh), L);
-    inv = f.x;
-    ty = f.y;
+    f = xent_norm(others, block_sum(own, sh), L);
+  } else {
+    f = xent_norm(sums[t].x, sums[t].y, L);
   }
   for (int v = threadIdx.x; v < ld; v += 256) {
     float p = 0.f;
-    if (v < n) {
-      if constexpr (WHOLE)
-        p = v == at ? ty : row[v] * inv;
-      else
-        p = expf(row[v] - L) - (v == at ? 1.f : 0.f);
-    }
+    if (v < n) p = v == at ? f.y : (WHOLE ? row[v] : expf(row[v] - L)) * f.x;
     row[v] = w != 0.f && v < n ? scale * (w * p) : 0.f;
   }
 }
@@ -628,14 +645,20 @@ hipError_t launch_xent_lse_f32(const float* l, int64_t ld, int T, int n, int v0,
   return hipGetLastError();
 }
 
-hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, bool whole, const float* lse, const XentTok& a,
-                              float scale, const void* H, void* Hm, int d, hipStream_t s) {
-  if (whole)
-    hipLaunchKernelGGL(k_xent_dl_f32<true>, dim3(T), dim3(256), 0, s, l, ld, n, v0, lse, a, scale, (const float4*)H,
-                       (float4*)Hm, d / 4);
+hipError_t launch_xent_sums_f32(const float* l, int64_t ld, int T, int n, int v0, const float* lse, const XentTok& a,
+                                float* sums, hipStream_t s) {
+  hipLaunchKernelGGL(k_xent_sums_f32, dim3(T), dim3(256), 0, s, l, ld, n, v0, lse, a, (float2*)sums);
+  return hipGetLastError();
+}
+
+hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, const float* sums, const float* lse,
+                              const XentTok& a, float scale, const void* H, void* Hm, int d, hipStream_t s) {
+  if (sums)
+    hipLaunchKernelGGL(k_xent_dl_f32<false>, dim3(T), dim3(256), 0, s, l, ld, n, v0, lse, (const float2*)sums, a, scale,
+                       (const float4*)H, (float4*)Hm, d / 4);
   else
-    hipLaunchKernelGGL(k_xent_dl_f32<false>, dim3(T), dim3(256), 0, s, l, ld, n, v0, lse, a, scale, (const float4*)H,
-                       (float4*)Hm, d / 4);
+    hipLaunchKernelGGL(k_xent_dl_f32<true>, dim3(T), dim3(256), 0, s, l, ld, n, v0, lse, nullptr, a, scale,
+                       (const float4*)H, (float4*)Hm, d / 4);
   return hipGetLastError();
 }
 

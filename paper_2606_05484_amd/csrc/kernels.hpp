@@ -403,9 +403,13 @@ hipError_t launch_xent_sum_dW(const float* part, int splits, int64_t n, float sc
 // with Hm H with the masked rows zero.
 hipError_t launch_xent_lse_f32(const float* l, int64_t ld, int T, int n, int v0, const XentTok& a, float* part, float* tgt,
                                hipStream_t s);
-// (whole: the piece is all of the vocabulary, normalised by its own sum.)
-hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, bool whole, const float* lse, const XentTok& a,
-                              float scale, const void* H, void* Hm, int d, hipStream_t s);
+// sums [T][2] of the exponentials exp(l - lse) over the pieces of a vocabulary, in turn from v0 = 0:
+// those that are no target's, and the target's.
+hipError_t launch_xent_sums_f32(const float* l, int64_t ld, int T, int n, int v0, const float* lse, const XentTok& a,
+                                float* sums, hipStream_t s);
+// (without sums the piece is all of the vocabulary.)
+hipError_t launch_xent_dl_f32(float* l, int64_t ld, int T, int n, int v0, const float* sums, const float* lse,
+                              const XentTok& a, float scale, const void* H, void* Hm, int d, hipStream_t s);
 hipError_t launch_xent_zero_rows(float* X, int T, int d, const XentTok& a, hipStream_t s);
 // flag[0] = 1 if any y[t] >= V.
 hipError_t launch_xent_check(const int32_t* y, int T, int64_t V, int* flag, hipStream_t s);

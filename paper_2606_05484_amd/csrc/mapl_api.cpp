@@ -1524,7 +1524,7 @@ constexpr int64_t kXentPieceBytes = (int64_t)512 << 20;
 constexpr int64_t kXentMaxPiece = (int64_t)1 << 21;  // columns (32-bit offsets inside a tile's panel)
 
 struct XentLayout {
-  size_t total = 0, flag = 0, part = 0, tgt = 0, tok = 0, hm = 0, dl = 0, acc = 0, accw = 0;
+  size_t total = 0, flag = 0, part = 0, tgt = 0, tok = 0, sums = 0, hm = 0, dl = 0, acc = 0, accw = 0;
   int64_t piece = 0, ld = 0;  // vocabulary entries per piece, a row of dl
   int64_t kper = 0, tper = 0;  // dH's run of K, dW's run of tokens
   int pieces = 1, splits = 1, tsplits = 1;
@@ -1574,6 +1574,7 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
     if (!bf) L.dl = c.take((size_t)T * L.ld * 4);
   } else {
     if (bf) L.tok = c.take((size_t)T * 8);
+    else if (L.pieces > 1) L.sums = c.take((size_t)T * 8);
     L.hm = c.take((size_t)T * D.d * es);
     L.dl = c.take((size_t)T * L.ld * es);
     if (bf) {
@@ -1750,12 +1751,19 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
 
   // ---------------- fp32 path: the vector loads take extents that are
   // multiples of 4; a piece's last one to three entries go on their own
-  float *l = at<float>(ws, L.dl), *Hm = at<float>(ws, L.hm);
-  for (int p = 0; p < L.pieces; ++p) {
+  float *l = at<float>(ws, L.dl), *Hm = at<float>(ws, L.hm), *sums = L.sums ? at<float>(ws, L.sums) : nullptr;
+  if (sums)  // a target's entry is the others' sum over all pieces: their logits once more
+    for (int p = 0; p < L.pieces; ++p) {
+      const int64_t v0 = p * L.piece, n = V - v0 < L.piece ? V - v0 : L.piece;
+      LAUNCH("xent_bwd:sum_logits", launch_gemm_f32(xent_logits_f32(D, H, W, v0, n, l, L.ld), s));
+      LAUNCH("xent_bwd:sums", launch_xent_sums_f32(l, L.ld, (int)T, (int)n, (int)v0, lse, a, sums, s));
+    }
+  for (int p = L.pieces - 1; p >= 0; --p) {  // the last piece first: the sums leave its logits in l
     const int64_t v0 = p * L.piece, n = V - v0 < L.piece ? V - v0 : L.piece;
-    LAUNCH("xent_bwd:logits", launch_gemm_f32(xent_logits_f32(D, H, W, v0, n, l, L.ld), s));
-    LAUNCH("xent_bwd:dl", launch_xent_dl_f32(l, L.ld, (int)T, (int)n, (int)v0, L.pieces == 1, lse, a, scale, H,
-                                              dW && p == 0 ? Hm : nullptr, (int)d, s));
+    const bool first = p == L.pieces - 1;
+    if (!sums || !first) LAUNCH("xent_bwd:logits", launch_gemm_f32(xent_logits_f32(D, H, W, v0, n, l, L.ld), s));
+    LAUNCH("xent_bwd:dl", launch_xent_dl_f32(l, L.ld, (int)T, (int)n, (int)v0, sums, lse, a, scale, H,
+                                              dW && first ? Hm : nullptr, (int)d, s));
     for (int64_t u0 = 0; u0 < n; u0 += n & ~(int64_t)3 ? n & ~(int64_t)3 : n) {
       const int64_t m = u0 == 0 && n >= 4 ? n & ~(int64_t)3 : n - u0;
       const float* Wp = (const float*)W + (v0 + u0) * d;
@@ -1764,7 +1772,7 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
         g.A = l + u0; g.sAm = L.ld; g.sAk = 1;
         g.B = Wp; g.sBk = d; g.sBn = 1;
         g.C = dH; g.sCm = d; g.sCn = 1;
-        if (v0 + u0 > 0) { g.Cin = (const float*)dH; g.sCinm = d; g.sCinn = 1; g.beta = 1.f; }
+        if (!first || u0 > 0) { g.Cin = (const float*)dH; g.sCinm = d; g.sCinn = 1; g.beta = 1.f; }
         LAUNCH("xent_bwd:dH", launch_gemm_f32(g, s));
       }
       if (dW) {

@@ -292,7 +292,8 @@ int mapl_ckpt_encode_bwd(const mapl_codec_desc* desc, const void* dZ, const int8
 size_t mapl_ckpt_encode_bwd_workspace_bytes(const mapl_codec_desc* desc);
 
 /* The last stage's loss: softmax cross entropy over the vocabulary of the
- * logits l[t,v] = sum_c H[t,c] W[v,c], which are never kept.
+ * logits l[t,v] = sum_c H[t,c] W[v,c], which are not kept (the fp32 calls hold
+ * those of a piece of the vocabulary in their workspace while they run).
  *   T tokens, 0 <= T <= 2^22; d, multiple of 64, 64 <= d <= 16384;
  *   V vocabulary entries, 1 <= V <= 2^22 (any, no multiple needed)
  *   x_dtype   MAPL_BF16 or MAPL_F32: H [T,d], W [V,d], dH [T,d]
@@ -320,9 +321,13 @@ size_t mapl_ckpt_encode_bwd_workspace_bytes(const mapl_codec_desc* desc);
  * bf16: logits, statistics and sums in fp32; dl is rounded to bf16 (before
  * scale, so that the 1 of a target stays exact) for its two products, and dW
  * in bf16 is rounded once per call.  Results are bitwise reproducible.
- * Workspace: mapl_xent_workspace_bytes(desc, MAPL_XENT_FWD or _BWD); the
- * backward's holds dl of a piece of the vocabulary at a time (512 MiB, or 512
- * bytes a token where that is more). */
+ * Workspace: mapl_xent_workspace_bytes(desc, MAPL_XENT_FWD or _BWD).  The fp32
+ * forward's holds the logits, and both backwards' dl, of a piece of the vocabulary
+ * at a time: all of it up to 512 MiB, else pieces of about that, or of 256 entries
+ * where that is more (512 bytes a token in bf16, 1024 in fp32).  The backward's also
+ * holds a copy of H; in bf16 fp32 sums of dH, [T, d] where the vocabulary has several
+ * pieces or up to 64 MiB where it is summed in runs, and up to 64 MiB of dW's sums over
+ * runs of tokens. */
 enum mapl_xent_call { MAPL_XENT_FWD = 0, MAPL_XENT_BWD = 1 };
 typedef struct mapl_xent_desc {
   int64_t T, d, V;

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) void k_ckpt_unpack(const uint4* __restrict__ q
 // traffic; the groups' sums meet in LDS at the end.  T = 32768, d = 2048, r = 256, 128
 // anchors: 47 us, 0.78 PFLOP/s; of these about 35 are its stages (1.1 us each, no
 // one of conversion, products, LDS reads or loads alone: without any one of them 4-8 us
-// less), the rest the partial sums (36 MB) and the start.  A wave converts the next
+// less), the rest the partial sums (33 MB) and the start.  A wave converts the next
 // stage's bytes under the first k-step's products and reads the next stage's first
 // fragments under the second's.
 constexpr int W8_BM = 128, W8_KT = 64, W8_THREADS = 512, W8_NS = 4;

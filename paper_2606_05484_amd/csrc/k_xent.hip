@@ -72,8 +72,8 @@ __device__ __forceinline__ void xent_from(int end, int lane, F&& f) {
 // C(m, n) = logit of vocabulary entry m, token n.  A wave reduces its 16 FM
 // vocabulary entries of each token in registers (the four lanes that share a
 // token meet by shuffles); the pair goes to part.  Bound by the products
-// (T = 32768, d = 2048, V = 32003 2.97 ms, 1.45 PFLOP/s), with few tokens by W's
-// bytes (T = 37, V = 32000 24 us, 5.5 TB/s).
+// (T = 32768, d = 2048, V = 32003 2.89 to 3.03 ms by the card, 1.49 to 1.42 PFLOP/s), with
+// few tokens by W's bytes (T = 37, V = 32000 24 us, 5.5 TB/s).
 template <class Cfg>
 XENT_KERNEL(Cfg) k_xent_lse(BgShape g, XentTok a, float2* part, float* tgt) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -204,8 +204,9 @@ __global__ __launch_bounds__(256) void k_xent_prep(const uint4* __restrict__ H, 
 
 // dl (bf16 [T][ld], columns past the piece zero) of the vocabulary piece that
 // starts at v0.  C(m, n) as in k_xent_lse.  Bound by the products and, after
-// them, by the exponentials (one a logit at a quarter of the vector rate: a quarter of a tile's
-// time at d = 1024).  T = 32768, d = 2048, V = 32000 3.2 ms, 1.35 PFLOP/s.
+// them, by the exponentials (one a logit at a quarter of the vector rate: at T = 8192,
+// d = 1024, V = 32000 a tenth of a launch, 453 us where dW's product of the same size takes 400).
+// T = 32768, d = 2048, V = 32000 3.2 ms, 1.35 PFLOP/s.
 template <class Cfg>
 XENT_KERNEL(Cfg) k_xent_dl(BgShape g, XentTok a, const float2* __restrict__ tok, int v0, bf16_t* __restrict__ dl, int64_t ld) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -1530,8 +1530,9 @@ struct XentLayout {
   int pieces = 1, splits = 1, tsplits = 1;
 };
 
-// A gradient product with fewer output tiles than CUs splits K into runs of
-// `per`, at least 512 deep and at most `most` of them: returns their number.
+// A gradient product with fewer output tiles than CUs splits K into equal runs
+// of `per`, one for every 512 begun (K = 513: 320 and 193) and at most `most`
+// of them: returns their number.
 int xent_runs(int64_t M, int64_t N, int64_t K, int64_t most, int64_t* per) {
   const int64_t tiles = (M + 255) / 256 * ((N + 255) / 256);
   int64_t s = tiles < 256 ? 256 / tiles : 1;
@@ -1578,12 +1579,13 @@ XentLayout xent_layout(const mapl_xent_desc& D, int call) {
     L.hm = c.take((size_t)T * D.d * es);
     L.dl = c.take((size_t)T * L.ld * es);
     if (bf) {
-      // dH has few output tiles: K split over the idle CUs, at least 512 deep (V = 32000, dH and its sum
+      // dH has few output tiles: K split over the idle CUs (V = 32000, dH and its sum
       // in us, unsplit, this, and a quarter of its runs: T = 37, d = 2048 252, 26 + 7, 39 + 7; d = 1024, T = 100 259, 20 + 10,
       // 25 + 8; T = 1021 271, 64 + 14, 82 + 7; T = 8192 508, 385 + 20, 507)
       L.splits = xent_runs(D.d, T, L.piece, 256, &L.kper);
-      // (a short vocabulary's runs would cost more, by their sum, than they save; by the
-      // model of xent_token_runs.  xent_bwd in us with its runs and with one, d = 1024:
+      // (a short vocabulary's runs would cost more, by their sum, than they save: modelled as in
+      // xent_token_runs, the sum's launch at 3 us and a run's sums at 1 us a million values, the
+      // constants that put these on their sides.  xent_bwd in us with its runs and with one, d = 1024:
       // V = 1000: T = 600 37.4, 34.0; T = 1021 43.2, 40.7; T = 8192 99.5, 80.9; V = 4000, T = 8192
       // 219, 203; the other way V = 1000: T = 500, d = 64 24.7, 26.3; T = 300, d = 256 25.9, 26.5)
       if (L.pieces == 1 && 0.48 / 64 * (double)D.V * (1.0 - 1.0 / L.splits) < 3.0 + 1e-6 * (double)(T * D.d) * L.splits)

@@ -340,6 +340,111 @@ int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const void* W, cons
                   void* stream);
 size_t mapl_xent_workspace_bytes(const mapl_xent_desc* desc, int call);
 
+/* The norms around a block of a stage, with the block's gate and residual scale:
+ * for every token (a row of d values; rms(z)_c = z_c / sqrt(mean z^2 + eps))
+ *   n  = rms(h) w_post          with MAPL_NORM_POST, else n = h
+ *   xo = x + alpha scale n act(gate)     with MAPL_NORM_BRANCH, else xo = x (not written)
+ *   y  = rms(xo) w_pre          with MAPL_NORM_PRE
+ * act: 1 (MAPL_GATE_NONE: gate is not read), sigmoid(gate), or gate sigmoid(gate).
+ *   parts  MAPL_NORM_PRE, MAPL_NORM_BRANCH, both, and MAPL_NORM_POST with the latter
+ *   T tokens, 0 <= T < 2^31; d, multiple of 64, 64 <= d <= 16384
+ *   ld_h, ld_gate  values from a row of h (dh) and of gate (dgate) to the next, a
+ *     multiple of 8, d <= ld <= 2^20; 0: d.  (h and gate may be the halves of one
+ *     product's [T, 2d].)  The other arrays are dense [T,d].
+ *   x_dtype   of x, xo, dxo, dx; h_dtype of h, gate, y, dy, dh, dgate: MAPL_BF16, or
+ *     MAPL_F32 where x_dtype is
+ *   w_post, scale, w_pre [d] fp32, each may be NULL: ones
+ *   1e-30 <= eps <= 1; alpha finite
+ * Everything in between is fp32; xo is rounded to its type before y is made of it.
+ * Rows of any finite size give finite results (their squares may overflow).
+ * mapl_norm_bwd, from the gradients dy of y (with MAPL_NORM_PRE) and dxo of xo (NULL: zeros;
+ * needed without MAPL_NORM_PRE); xo is what the forward wrote (x without a branch; not
+ * read without MAPL_NORM_PRE):
+ *   dx = dxo + the gradient through y: of x, and of xo in what follows.  Written with
+ *     MAPL_NORM_PRE; else it is dxo itself, and dx has to be NULL
+ *   dh, dgate  with a branch (dgate with a gate); rows of ld_h and ld_gate
+ *   dw_post, dscale, dw_pre [d] fp32 (+)= the vectors' gradients, each may be NULL: left
+ *     out.  accumulate_dw = 0 overwrites them, 1 adds to them
+ * Arrays that `parts` leaves out are not read or written, and have to be NULL.
+ * Results are bitwise reproducible.  Workspace: mapl_norm_workspace_bytes (the backward's). */
+enum mapl_norm_part { MAPL_NORM_PRE = 1, MAPL_NORM_BRANCH = 2, MAPL_NORM_POST = 4 };
+enum mapl_gate { MAPL_GATE_NONE = 0, MAPL_GATE_SIGMOID = 1, MAPL_GATE_SILU = 2 };
+typedef struct mapl_norm_desc {
+  int64_t T, d, ld_h, ld_gate;
+  int32_t x_dtype, h_dtype, parts, gate;
+  float alpha, eps;
+} mapl_norm_desc;
+int mapl_norm_fwd(const mapl_norm_desc* desc, const void* x, const void* h, const void* gate, const float* w_post,
+                  const float* scale, const float* w_pre, void* xo, void* y, void* stream);
+int mapl_norm_bwd(const mapl_norm_desc* desc, const void* dy, const void* dxo, const void* xo, const void* h,
+                  const void* gate, const float* w_post, const float* scale, const float* w_pre, void* dx, void* dh,
+                  void* dgate, float* dw_post, float* dscale, float* dw_pre, int accumulate_dw, void* ws,
+                  size_t ws_bytes, void* stream);
+size_t mapl_norm_workspace_bytes(const mapl_norm_desc* desc);
+
+/* The optimizer's step over all tensors of a stage at once (the paper's AdamW for what
+ * is neither a projector nor its other optimizer's).  `params` is a HOST array of
+ * `count` tensors (0 <= count <= 2^20), read during the call; its pointers are device
+ * pointers, and each call says which of them it uses.
+ *   n values, 0 <= n <= 2^38; g [n] of g_dtype (MAPL_BF16 or MAPL_F32); p [n] fp32
+ *   m, v   states: MAPL_STATES_F32 fp32 [n] each; MAPL_STATES_8BIT one byte a value
+ *   e      8 bits: [ceil(n/128)][2] exponent bytes (m's, then sqrt(v)'s); else not used
+ *   p16    [n] bf16, may be NULL: p's new values rounded (what the next forward reads)
+ *   weight_decay, lr_scale  this tensor's (lr is multiplied by lr_scale), finite
+ * No output may overlap any other array of the call, the same tensor twice included.
+ *
+ * mapl_grad_norm (uses n, g):
+ *   stats[0] = |grad_scale| sqrt(sum of all g^2)        stats [2] fp32
+ *   stats[1] = grad_scale min(1, max_norm / stats[0])   what clips them (max_norm > 0, INFINITY: never)
+ *   step[0] += 1 where stats[0] is finite               step int32, may be NULL
+ * The sum is in 64 bits.  Workspace: mapl_grad_norm_workspace_bytes.
+ *
+ * mapl_adamw_step (uses all of them), with g' = stats[1] g (stats NULL: g' = g):
+ *   m <- m + (1 - beta1) (g' - m),  v <- v + (1 - beta2) (g'^2 - v)
+ *   p <- p - (lr wd p + lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps))
+ * stats, as mapl_grad_norm leaves it: where stats[0] is not finite nothing is changed.
+ * t >= 1 is step[0] on the device, or desc's step where step is NULL; lr is lr[0] on the
+ * device, or desc's where lr is NULL (a captured graph keeps desc's values of the
+ * capture, and reads step and lr anew in every replay).
+ * 0 <= beta1, beta2 < 1; eps > 0; lr, eps finite.  fp32 arithmetic.
+ * MAPL_STATES_8BIT: m is kept with 4 exponent and 3 mantissa bits (float8_e4m3fn's
+ * values) times 2^(byte-135), s = sqrt(v) with 4 and 4 bits (no sign) times 2^(byte-127);
+ * a block of 128 values shares the two bytes, the least (but at least 24) for which
+ * 1.75 2^(byte-127) holds m's largest magnitude and 1.9375 2^(byte-127) s's.  Code c of s
+ * stands for (16 + c % 16) 2^(c/16 - 19), c < 16: c 2^-18.  All bytes zero is the start
+ * (m = v = 0).  The step uses m and v before they are rounded.  They are rounded up or
+ * down at random with the mean at the value, by the bits of a hash of (seed, t, the
+ * tensor's place in params, i mod 2^32), so the same call gives the same bits; an s
+ * above 0 never becomes 0.  What is rounded is the fp32 result of the two lines
+ * above, every operation rounded to nearest, and the root.  A block that holds a NaN, an
+ * infinity or a magnitude past 1.75 2^127 stands for NaNs.
+ *
+ * mapl_adamw_unpack writes the values of the 8-bit states of `packed` (uses n, m, v, e)
+ * as fp32 into m and v of `values` (uses n, m, v; the same count and n), and
+ * mapl_adamw_pack the other way, rounded to nearest. */
+enum mapl_states { MAPL_STATES_F32 = 0, MAPL_STATES_8BIT = 1 };
+typedef struct mapl_param {
+  int64_t n;
+  const void* g;
+  float* p;
+  void *m, *v;
+  uint8_t* e;
+  void* p16;
+  float weight_decay, lr_scale;
+} mapl_param;
+typedef struct mapl_adamw_desc {
+  float lr, beta1, beta2, eps;
+  int32_t g_dtype, states, step;
+  uint32_t seed;
+} mapl_adamw_desc;
+int mapl_grad_norm(const mapl_param* params, int64_t count, int32_t g_dtype, float grad_scale, float max_norm,
+                   float* stats, int32_t* step, void* ws, size_t ws_bytes, void* stream);
+size_t mapl_grad_norm_workspace_bytes(const mapl_param* params, int64_t count, int32_t g_dtype);
+int mapl_adamw_step(const mapl_adamw_desc* desc, const mapl_param* params, int64_t count, const float* stats,
+                    const int32_t* step, const float* lr, void* stream);
+int mapl_adamw_unpack(const mapl_param* packed, const mapl_param* values, int64_t count, void* stream);
+int mapl_adamw_pack(const mapl_param* values, const mapl_param* packed, int64_t count, void* stream);
+
 /* mapl_encode without a workspace, for callers that cannot allocate device
  * memory (code under HIP graph capture, tight serving loops, harnesses that
  * forbid hipMalloc).  Same arguments, results and errors as mapl_encode;

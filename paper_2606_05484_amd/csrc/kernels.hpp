@@ -414,6 +414,64 @@ hipError_t launch_xent_zero_rows(float* X, int T, int d, const XentTok& a, hipSt
 // flag[0] = 1 if any y[t] >= V.
 hipError_t launch_xent_check(const int32_t* y, int T, int64_t V, int* flag, hipStream_t s);
 
+// ---------------------------------------------------------------- norms around a block
+enum { NORM_PRE = 1, NORM_BRANCH = 2, NORM_POST = 4 };  // the values of MAPL_NORM_*
+enum { NORM_SIGMOID = 1, NORM_SILU = 2 };               // those of MAPL_GATE_*
+// x, xo, dxo, dx [T][d] bf16 or fp32; h, dh rows of ld_h, gate, dgate rows of ld_g,
+// y, dy [T][d], bf16 or (with an fp32 x) fp32; vectors [d] fp32, null for ones.
+// The backward's x is the forward's xo (x without a branch); gate null: none.
+// part: see norm_bwd_parts; null: no gradients of the vectors.
+struct NormArgs {
+  int64_t T, ld_h, ld_g;
+  int d, parts, act, x_f32, h_f32;
+  float alpha, eps;
+  const void *x, *h, *gate, *dy, *dxo;
+  const float *w_post, *scale, *w_pre;
+  void *xo, *y, *dx, *dh, *dgate;
+  float* part;
+};
+hipError_t launch_norm_fwd(const NormArgs& g, hipStream_t s);
+// T >= 1; leaves part [norm_bwd_parts(T, d)][3][d] fp32 (dw_post, dscale, dw_pre).
+int norm_bwd_parts(int64_t T, int d);
+hipError_t launch_norm_bwd(const NormArgs& g, hipStream_t s);
+struct NormSums {
+  float *dw_post, *dscale, *dw_pre;  // [d], null: left out
+};
+hipError_t launch_norm_sum(const float* part, int n, int d, const NormSums& o, int add, hipStream_t s);
+
+// ---------------------------------------------------------------- optimizer
+// One tensor of a step; a launch takes up to OPTIM_TENSORS of them in its
+// arguments (no table in memory that would have to be copied or outlive the call).
+struct OptimTensor {
+  float* p; const void* g; void* m; void* v; uint8_t* e; bf16_t* p16;
+  int64_t n;
+  float weight_decay, lr_scale;
+};
+constexpr int OPTIM_TENSORS = 52;
+struct OptimTable {
+  OptimTensor t[OPTIM_TENSORS];
+  uint32_t first[OPTIM_TENSORS + 1];  // the workgroups' pieces: tensor i has first[i] .. first[i + 1] - 1
+  int count;
+  uint32_t index;  // the first tensor's in the whole call
+};
+int64_t optim_pieces(int64_t n);
+// part[0 .. grad_norm_parts(pieces) - 1]: sums of squares (64 bits)
+int grad_norm_parts(int64_t pieces);
+hipError_t launch_grad_squares(const OptimTable& t, int g_f32, double* part, hipStream_t s);
+hipError_t launch_grad_norm(const double* part, int n, float grad_scale, float max_norm, float* stats, int32_t* step,
+                            hipStream_t s);
+struct AdamwArgs {
+  float lr, eps, c1, c2, ln_b1, ln_b2;  // c = 1 - b, ln_b = log b
+  int g_f32, low, step;
+  uint32_t seed;
+  const float *stats, *lr_at;
+  const int32_t* step_at;
+};
+hipError_t launch_adamw(const OptimTable& t, const AdamwArgs& a, hipStream_t s);
+// 8-bit states (t's m, v, e) and fp32 ones (t's p and, in place of g, v) of each tensor
+hipError_t launch_adamw_unpack(const OptimTable& t, hipStream_t s);
+hipError_t launch_adamw_pack(const OptimTable& t, hipStream_t s);
+
 // ---------------------------------------------------------------- debug
 // flag[0] = 1 if any ids[t] is outside [0, V).
 hipError_t launch_check_ids(const int32_t* ids, int T, int64_t V, int* flag, hipStream_t s);

@@ -15,6 +15,7 @@
 //               Eq. 7 retraction by PolarExpress, batched over projectors.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -22,6 +23,7 @@
 #include <cstring>
 #include <map>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -1790,6 +1792,391 @@ extern "C" int mapl_xent_bwd(const mapl_xent_desc* desc, const void* H, const vo
   }
   if (dH) LAUNCH("xent_bwd:mask", launch_xent_zero_rows((float*)dH, (int)T, (int)d, a, s));
   return MAPL_OK;
+}
+
+// ---------------------------------------------------- norms around a block
+namespace {
+struct NormLayout {
+  size_t total = 0, part = 0;
+};
+NormLayout norm_layout(const mapl_norm_desc& D) {
+  NormLayout L;
+  Carve c;
+  L.part = c.take((size_t)norm_bwd_parts(D.T > 0 ? D.T : 1, (int)D.d) * 3 * D.d * 4);
+  L.total = c.off;
+  return L;
+}
+
+int check_norm(const mapl_norm_desc* D) {
+  if (!D) return fail(MAPL_E_NULL, "desc is NULL");
+  if (D->x_dtype != MAPL_BF16 && D->x_dtype != MAPL_F32)
+    return fail(MAPL_E_DTYPE, "x_dtype must be MAPL_BF16 or MAPL_F32 (got %d)", D->x_dtype);
+  if (D->h_dtype != MAPL_BF16 && !(D->h_dtype == MAPL_F32 && D->x_dtype == MAPL_F32))
+    return fail(MAPL_E_DTYPE, "h_dtype must be MAPL_BF16, or MAPL_F32 where x_dtype is (got %d)", D->h_dtype);
+  if (D->T < 0 || D->T >= ((int64_t)1 << 31)) return fail(MAPL_E_SHAPE, "T=%lld out of range", (long long)D->T);
+  if (D->d < 64 || D->d > 16384 || D->d % 64)
+    return fail(MAPL_E_SHAPE, "d=%lld: need 64 <= d <= 16384, d %% 64 == 0", (long long)D->d);
+  for (const int64_t ld : {D->ld_h, D->ld_gate})
+    if (ld != 0 && (ld < D->d || ld > ((int64_t)1 << 20) || ld % 8))
+      return fail(MAPL_E_SHAPE, "a row stride of %lld: need 0, or d <= ld <= 2^20, ld %% 8 == 0", (long long)ld);
+  const int p = D->parts;
+  if (p != (p & 7) || !(p & (MAPL_NORM_PRE | MAPL_NORM_BRANCH)) || ((p & MAPL_NORM_POST) && !(p & MAPL_NORM_BRANCH)))
+    return fail(MAPL_E_SHAPE, "parts=%d: need MAPL_NORM_PRE or MAPL_NORM_BRANCH, and MAPL_NORM_POST only with the latter", p);
+  if (D->gate < MAPL_GATE_NONE || D->gate > MAPL_GATE_SILU) return fail(MAPL_E_SHAPE, "gate=%d unknown", D->gate);
+  if (D->gate != MAPL_GATE_NONE && !(p & MAPL_NORM_BRANCH)) return fail(MAPL_E_SHAPE, "a gate needs MAPL_NORM_BRANCH");
+  if (!(D->eps >= 1e-30f && D->eps <= 1.f)) return fail(MAPL_E_SHAPE, "eps=%g: need 1e-30 <= eps <= 1", (double)D->eps);
+  if (!std::isfinite(D->alpha)) return fail(MAPL_E_SHAPE, "alpha is not finite");
+  return MAPL_OK;
+}
+
+// bytes from the first to the last value of T rows, ld apart (0: dense)
+size_t rows_bytes(const mapl_norm_desc& D, int64_t ld) {
+  return D.T == 0 ? 0 : (size_t)((D.T - 1) * (ld ? ld : D.d) + D.d) * esize(D.h_dtype);
+}
+
+// Rows of two arrays may lie between each other's (the halves of one [T, 2d]):
+// whether any of a's d values a row are among b's, ld values apart in both.
+bool rows_overlap(const void* a, const void* b, size_t bytes_a, size_t bytes_b, int64_t ld_a, int64_t ld_b, int64_t d,
+                  size_t es) {
+  if (!a || !b || !bytes_a || !bytes_b) return false;
+  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+  if (a0 + bytes_a <= b0 || b0 + bytes_b <= a0) return false;
+  if (ld_a != ld_b || ld_a == d) return true;
+  const uintptr_t row = (uintptr_t)ld_a * es, len = (uintptr_t)d * es;
+  const uintptr_t off = (a0 > b0 ? a0 - b0 : b0 - a0) % row;  // the later array's row inside the earlier one's
+  return off < len || off + len > row;
+}
+
+int only_with(bool on, std::initializer_list<Span> s, const char* what) {
+  if (!on)
+    for (const Span& x : s)
+      if (x.p) return fail(MAPL_E_SHAPE, "%s has to be NULL without %s", x.name, what);
+  return MAPL_OK;
+}
+
+NormArgs norm_args(const mapl_norm_desc& D) {
+  NormArgs g{};
+  g.T = D.T; g.d = (int)D.d;
+  g.ld_h = D.ld_h ? D.ld_h : D.d; g.ld_g = D.ld_gate ? D.ld_gate : D.d;
+  g.parts = D.parts; g.act = D.gate;
+  g.x_f32 = D.x_dtype == MAPL_F32; g.h_f32 = D.h_dtype == MAPL_F32;
+  g.alpha = D.alpha; g.eps = D.eps;
+  return g;
+}
+}  // namespace
+
+extern "C" size_t mapl_norm_workspace_bytes(const mapl_norm_desc* desc) {
+  g_err.clear();
+  if (check_norm(desc) != MAPL_OK) return 0;
+  return norm_layout(*desc).total;
+}
+
+extern "C" int mapl_norm_fwd(const mapl_norm_desc* desc, const void* x, const void* h, const void* gate,
+                             const float* w_post, const float* scale, const float* w_pre, void* xo, void* y,
+                             void* stream) {
+  g_err.clear();
+  int st = check_norm(desc);
+  if (st) return st;
+  const mapl_norm_desc& D = *desc;
+  const bool br = D.parts & MAPL_NORM_BRANCH, post = D.parts & MAPL_NORM_POST, pre = D.parts & MAPL_NORM_PRE;
+  const bool gated = D.gate != MAPL_GATE_NONE;
+  const size_t xb = (size_t)D.T * D.d * esize(D.x_dtype), yb = (size_t)D.T * D.d * esize(D.h_dtype), vb = (size_t)D.d * 4;
+  const size_t hb = rows_bytes(D, D.ld_h), gb = rows_bytes(D, D.ld_gate);
+  st = only_with(br, {{h, 0, "h"}, {scale, 0, "scale"}, {xo, 0, "xo"}}, "MAPL_NORM_BRANCH");
+  if (!st) st = only_with(post, {{w_post, 0, "w_post"}}, "MAPL_NORM_POST");
+  if (!st) st = only_with(pre, {{w_pre, 0, "w_pre"}, {y, 0, "y"}}, "MAPL_NORM_PRE");
+  if (!st) st = only_with(gated, {{gate, 0, "gate"}}, "a gate");
+  if (st) return st;
+  st = check_ptrs({{x, xb, "x"}, {h, br ? hb : 0, "h"}, {gate, gated ? gb : 0, "gate"}, {w_post, 0, "w_post"},
+                   {scale, 0, "scale"}, {w_pre, 0, "w_pre"}, {xo, br ? xb : 0, "xo"}, {y, pre ? yb : 0, "y"}},
+                  {{xo, xb, "xo"}, {y, yb, "y"}},
+                  {{x, xb, "x"}, {h, hb, "h"}, {gate, gb, "gate"}, {w_post, vb, "w_post"}, {scale, vb, "scale"},
+                   {w_pre, vb, "w_pre"}});
+  if (!st) st = check_ptrs({}, {{xo, xb, "xo"}}, {{y, yb, "y"}});
+  if (st) return st;
+  if (D.T == 0) return MAPL_OK;
+  NormArgs g = norm_args(D);
+  g.x = x; g.h = h; g.gate = gate; g.w_post = w_post; g.scale = scale; g.w_pre = w_pre;
+  g.xo = xo; g.y = y;
+  hipStream_t s = (hipStream_t)stream;
+  LAUNCH("norm:fwd", launch_norm_fwd(g, s));
+  return MAPL_OK;
+}
+
+extern "C" int mapl_norm_bwd(const mapl_norm_desc* desc, const void* dy, const void* dxo, const void* xo, const void* h,
+                             const void* gate, const float* w_post, const float* scale, const float* w_pre, void* dx,
+                             void* dh, void* dgate, float* dw_post, float* dscale, float* dw_pre, int accumulate_dw,
+                             void* ws, size_t ws_bytes, void* stream) {
+  g_err.clear();
+  int st = check_norm(desc);
+  if (st) return st;
+  const mapl_norm_desc& D = *desc;
+  const bool br = D.parts & MAPL_NORM_BRANCH, post = D.parts & MAPL_NORM_POST, pre = D.parts & MAPL_NORM_PRE;
+  const bool gated = D.gate != MAPL_GATE_NONE;
+  const size_t xb = (size_t)D.T * D.d * esize(D.x_dtype), yb = (size_t)D.T * D.d * esize(D.h_dtype), vb = (size_t)D.d * 4;
+  const size_t hb = rows_bytes(D, D.ld_h), gb = rows_bytes(D, D.ld_gate), es = esize(D.h_dtype);
+  st = only_with(br, {{h, 0, "h"}, {scale, 0, "scale"}, {dh, 0, "dh"}, {dscale, 0, "dscale"}}, "MAPL_NORM_BRANCH");
+  if (!st) st = only_with(post, {{w_post, 0, "w_post"}, {dw_post, 0, "dw_post"}}, "MAPL_NORM_POST");
+  if (!st) st = only_with(pre, {{dy, 0, "dy"}, {xo, 0, "xo"}, {w_pre, 0, "w_pre"}, {dx, 0, "dx"}, {dw_pre, 0, "dw_pre"}},
+                          "MAPL_NORM_PRE");
+  if (!st) st = only_with(gated, {{gate, 0, "gate"}, {dgate, 0, "dgate"}}, "a gate");
+  if (st) return st;
+  st = check_ptrs({{dy, pre ? yb : 0, "dy"}, {dxo, pre ? 0 : xb, "dxo"}, {xo, pre ? xb : 0, "xo"}, {h, br ? hb : 0, "h"},
+                   {gate, gated ? gb : 0, "gate"}, {w_post, 0, "w_post"}, {scale, 0, "scale"}, {w_pre, 0, "w_pre"},
+                   {dx, pre ? xb : 0, "dx"}, {dh, br ? hb : 0, "dh"}, {dgate, gated ? gb : 0, "dgate"},
+                   {dw_post, 0, "dw_post"}, {dscale, 0, "dscale"}, {dw_pre, 0, "dw_pre"}},
+                  {{dx, xb, "dx"}, {dh, hb, "dh"}, {dgate, gb, "dgate"}, {dw_post, vb, "dw_post"}, {dscale, vb, "dscale"},
+                   {dw_pre, vb, "dw_pre"}},
+                  {{dy, yb, "dy"}, {dxo, xb, "dxo"}, {xo, xb, "xo"}, {h, hb, "h"}, {gate, gb, "gate"},
+                   {w_post, vb, "w_post"}, {scale, vb, "scale"}, {w_pre, vb, "w_pre"}, {ws, ws_bytes, "workspace"}});
+  if (!st) st = check_ptrs({}, {{dx, xb, "dx"}}, {{dh, hb, "dh"}, {dgate, gb, "dgate"}});
+  if (!st)
+    st = check_ptrs({}, {{dw_post, vb, "dw_post"}, {dscale, vb, "dscale"}, {dw_pre, vb, "dw_pre"}},
+                    {{dx, xb, "dx"}, {dh, hb, "dh"}, {dgate, gb, "dgate"}});
+  if (!st) st = check_ptrs({}, {{dw_post, vb, "dw_post"}}, {{dscale, vb, "dscale"}, {dw_pre, vb, "dw_pre"}});
+  if (!st) st = check_ptrs({}, {{dscale, vb, "dscale"}}, {{dw_pre, vb, "dw_pre"}});
+  if (st) return st;
+  NormArgs g = norm_args(D);
+  if (rows_overlap(dh, dgate, hb, gb, g.ld_h, g.ld_g, D.d, es)) return fail(MAPL_E_ALIAS, "output dh overlaps output dgate");
+  const NormLayout L = norm_layout(D);
+  if ((st = check_ws(ws, ws_bytes, L.total))) return st;
+  hipStream_t s = (hipStream_t)stream;
+  const NormSums o{dw_post, dscale, dw_pre};
+  const bool sums = dw_post || dscale || dw_pre;
+  const int n = D.T ? norm_bwd_parts(D.T, (int)D.d) : 0;
+  if (D.T) {
+    g.x = xo; g.h = h; g.gate = gate; g.dy = dy; g.dxo = dxo;
+    g.w_post = w_post; g.scale = scale; g.w_pre = w_pre;
+    g.dx = dx; g.dh = dh; g.dgate = dgate;
+    g.part = sums ? at<float>(ws, L.part) : nullptr;
+    LAUNCH("norm:bwd", launch_norm_bwd(g, s));
+  }
+  if (sums && (D.T || !accumulate_dw))
+    LAUNCH("norm:sum", launch_norm_sum(at<float>(ws, L.part), n, (int)D.d, o, accumulate_dw ? 1 : 0, s));
+  return MAPL_OK;
+}
+
+// ------------------------------------------------------------- optimizer step
+namespace {
+constexpr int64_t kMaxParams = (int64_t)1 << 20, kMaxValues = (int64_t)1 << 38;
+
+// Every array of a call with its extent, to be looked through for overlaps: an
+// output with anything, the same tensor given twice included.
+struct Extents {
+  struct X {
+    uintptr_t lo, hi;
+    bool out;
+    const char* name;
+    int64_t of;
+  };
+  std::vector<X> all;
+  int64_t of = -1;  // the tensor whose arrays are being added
+  int st = MAPL_OK;
+  void add(const void* p, int64_t bytes, const char* name, bool out, bool need = true) {
+    if (st || bytes == 0 || (!p && !need)) return;
+    char where[32] = "";
+    if (of >= 0) snprintf(where, sizeof where, "params[%lld].", (long long)of);
+    if (!p)
+      st = fail(MAPL_E_NULL, "%s%s is NULL", where, name);
+    else if (!aligned(p, 16))
+      st = fail(MAPL_E_ALIGN, "%s%s is not 16-byte aligned", where, name);
+    else
+      all.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, out, name, of});
+  }
+  int check() {
+    if (st) return st;
+    std::sort(all.begin(), all.end(), [](const X& a, const X& b) { return a.lo < b.lo; });
+    const X *far = nullptr, *far_out = nullptr;  // those that reach furthest
+    for (const X& x : all) {
+      const X* y = x.out && far && far->hi > x.lo ? far : far_out && far_out->hi > x.lo ? far_out : nullptr;
+      if (y)
+        return fail(MAPL_E_ALIAS, "%s (tensor %lld) overlaps %s (tensor %lld)", x.out ? x.name : y->name,
+                    (long long)(x.out ? x.of : y->of), x.out ? y->name : x.name, (long long)(x.out ? y->of : x.of));
+      if (!far || x.hi > far->hi) far = &x;
+      if (x.out && (!far_out || x.hi > far_out->hi)) far_out = &x;
+    }
+    return MAPL_OK;
+  }
+};
+
+int check_params(const mapl_param* params, int64_t count) {
+  if (count < 0 || count > kMaxParams) return fail(MAPL_E_SHAPE, "count=%lld: need 0 <= count <= 2^20", (long long)count);
+  if (!params && count > 0) return fail(MAPL_E_NULL, "params is NULL");
+  for (int64_t i = 0; i < count; ++i) {
+    if (params[i].n < 0 || params[i].n > kMaxValues)
+      return fail(MAPL_E_SHAPE, "params[%lld].n=%lld: need 0 <= n <= 2^38", (long long)i, (long long)params[i].n);
+  }
+  return MAPL_OK;
+}
+int check_g_dtype(int g_dtype) {
+  if (g_dtype != MAPL_BF16 && g_dtype != MAPL_F32)
+    return fail(MAPL_E_DTYPE, "g_dtype must be MAPL_BF16 or MAPL_F32 (got %d)", g_dtype);
+  return MAPL_OK;
+}
+
+// Calls f(table) for the tensors in turn, as many as a launch takes at a time.
+template <typename F>
+int for_tables(const mapl_param* params, const mapl_param* values, int64_t count, F&& f) {
+  OptimTable t;
+  for (int64_t i = 0; i < count;) {
+    t.count = 0;
+    t.index = (uint32_t)i;
+    t.first[0] = 0;
+    for (; t.count < OPTIM_TENSORS && i < count; ++i) {
+      const mapl_param& p = params[i];
+      if (t.count && t.first[t.count] + optim_pieces(p.n) > ((int64_t)1 << 30)) break;
+      t.t[t.count] = {p.p, p.g, p.m, p.v, p.e, (bf16_t*)p.p16, p.n, p.weight_decay, p.lr_scale};
+      if (values) t.t[t.count].p = (float*)values[i].m, t.t[t.count].g = values[i].v;
+      t.first[t.count + 1] = t.first[t.count] + (uint32_t)optim_pieces(p.n);
+      ++t.count;
+    }
+    if (t.first[t.count] == 0) continue;
+    const int st = f(t);
+    if (st) return st;
+  }
+  return MAPL_OK;
+}
+
+int64_t grad_parts(const mapl_param* params, int64_t count) {
+  int64_t n = 0;
+  for_tables(params, nullptr, count, [&](const OptimTable& t) {
+    n += grad_norm_parts(t.first[t.count]);
+    return (int)MAPL_OK;
+  });
+  return n;
+}
+
+int convert_states(const mapl_param* packed, const mapl_param* values, int64_t count, bool pack, void* stream) {
+  g_err.clear();
+  int st = check_params(packed, count);
+  if (!st) st = check_params(values, count);
+  if (st) return st;
+  try {
+    Extents x;
+    for (int64_t i = 0; i < count; ++i) {
+      const mapl_param &q = packed[i], &u = values[i];
+      if (q.n != u.n)
+        return fail(MAPL_E_SHAPE, "tensor %lld has %lld values packed and %lld unpacked", (long long)i, (long long)q.n, (long long)u.n);
+      x.of = i;
+      x.add(q.m, q.n, "m", pack);
+      x.add(q.v, q.n, "v", pack);
+      x.add(q.e, (q.n + 127) / 128 * 2, "e", pack);
+      x.add(u.m, 4 * q.n, "m (fp32)", !pack);
+      x.add(u.v, 4 * q.n, "v (fp32)", !pack);
+    }
+    if ((st = x.check())) return st;
+  } catch (const std::bad_alloc&) {
+    return fail(MAPL_E_UNSUPPORTED, "no host memory to check %lld tensors", (long long)count);
+  }
+  hipStream_t s = (hipStream_t)stream;
+  return for_tables(packed, values, count, [&](const OptimTable& t) {
+    if (pack)
+      LAUNCH("adamw:pack", launch_adamw_pack(t, s));
+    else
+      LAUNCH("adamw:unpack", launch_adamw_unpack(t, s));
+    return (int)MAPL_OK;
+  });
+}
+}  // namespace
+
+extern "C" size_t mapl_grad_norm_workspace_bytes(const mapl_param* params, int64_t count, int32_t g_dtype) {
+  g_err.clear();
+  if (check_params(params, count) != MAPL_OK || check_g_dtype(g_dtype) != MAPL_OK) return 0;
+  return (size_t)rup(8 * grad_parts(params, count), 256) + 256;
+}
+
+extern "C" int mapl_grad_norm(const mapl_param* params, int64_t count, int32_t g_dtype, float grad_scale, float max_norm,
+                              float* stats, int32_t* step, void* ws, size_t ws_bytes, void* stream) {
+  g_err.clear();
+  int st = check_params(params, count);
+  if (!st) st = check_g_dtype(g_dtype);
+  if (st) return st;
+  if (!std::isfinite(grad_scale)) return fail(MAPL_E_SHAPE, "grad_scale is not finite");
+  if (!(max_norm > 0.f)) return fail(MAPL_E_SHAPE, "max_norm=%g: need a positive number, or infinity", (double)max_norm);
+  const size_t need = (size_t)rup(8 * grad_parts(params, count), 256) + 256;
+  if (!stats) return fail(MAPL_E_NULL, "stats is NULL");
+  if ((st = check_ws(ws, ws_bytes, need))) return st;
+  try {
+    Extents x;
+    x.add(stats, 8, "stats", true);
+    x.add(step, 4, "step", true, false);
+    x.add(ws, (int64_t)ws_bytes, "workspace", true);
+    for (int64_t i = 0; i < count; ++i) {
+      x.of = i;
+      x.add(params[i].g, params[i].n * (int64_t)esize(g_dtype), "g", false);
+    }
+    if ((st = x.check())) return st;
+  } catch (const std::bad_alloc&) {
+    return fail(MAPL_E_UNSUPPORTED, "no host memory to check %lld tensors", (long long)count);
+  }
+  hipStream_t s = (hipStream_t)stream;
+  double* part = (double*)ws;
+  int64_t n = 0;
+  st = for_tables(params, nullptr, count, [&](const OptimTable& t) {
+    LAUNCH("grad_norm:squares", launch_grad_squares(t, g_dtype == MAPL_F32, part + n, s));
+    n += grad_norm_parts(t.first[t.count]);
+    return (int)MAPL_OK;
+  });
+  if (st) return st;
+  LAUNCH("grad_norm:norm", launch_grad_norm(part, (int)n, grad_scale, max_norm, stats, step, s));
+  return MAPL_OK;
+}
+
+extern "C" int mapl_adamw_step(const mapl_adamw_desc* desc, const mapl_param* params, int64_t count, const float* stats,
+                               const int32_t* step, const float* lr, void* stream) {
+  g_err.clear();
+  if (!desc) return fail(MAPL_E_NULL, "desc is NULL");
+  const mapl_adamw_desc& D = *desc;
+  int st = check_params(params, count);
+  if (!st) st = check_g_dtype(D.g_dtype);
+  if (st) return st;
+  if (D.states != MAPL_STATES_F32 && D.states != MAPL_STATES_8BIT) return fail(MAPL_E_DTYPE, "states=%d unknown", D.states);
+  if (!(D.beta1 >= 0.f && D.beta1 < 1.f && D.beta2 >= 0.f && D.beta2 < 1.f))
+    return fail(MAPL_E_SHAPE, "beta1=%g, beta2=%g: need 0 <= beta < 1", (double)D.beta1, (double)D.beta2);
+  if (!(D.eps > 0.f) || !std::isfinite(D.eps)) return fail(MAPL_E_SHAPE, "eps=%g: need a positive number", (double)D.eps);
+  if (!lr && !std::isfinite(D.lr)) return fail(MAPL_E_SHAPE, "lr is not finite");
+  if (!step && D.step < 1) return fail(MAPL_E_SHAPE, "step=%d: the first step is 1", D.step);
+  const bool low = D.states == MAPL_STATES_8BIT;
+  try {
+    Extents x;
+    x.add(stats, 8, "stats", false, false);
+    x.add(step, 4, "step", false, false);
+    x.add(lr, 4, "lr", false, false);
+    for (int64_t i = 0; i < count; ++i) {
+      const mapl_param& p = params[i];
+      if (!std::isfinite(p.weight_decay) || !std::isfinite(p.lr_scale))
+        return fail(MAPL_E_SHAPE, "params[%lld]: weight_decay or lr_scale is not finite", (long long)i);
+      x.of = i;
+      x.add(p.g, p.n * (int64_t)esize(D.g_dtype), "g", false);
+      x.add(p.p, 4 * p.n, "p", true);
+      x.add(p.m, low ? p.n : 4 * p.n, "m", true);
+      x.add(p.v, low ? p.n : 4 * p.n, "v", true);
+      if (low) x.add(p.e, (p.n + 127) / 128 * 2, "e", true);
+      x.add(p.p16, 2 * p.n, "p16", true, false);
+    }
+    if ((st = x.check())) return st;
+  } catch (const std::bad_alloc&) {
+    return fail(MAPL_E_UNSUPPORTED, "no host memory to check %lld tensors", (long long)count);
+  }
+  AdamwArgs a{};
+  a.lr = D.lr; a.eps = D.eps;
+  a.c1 = (float)(1.0 - (double)D.beta1); a.c2 = (float)(1.0 - (double)D.beta2);
+  a.ln_b1 = (float)std::log((double)D.beta1); a.ln_b2 = (float)std::log((double)D.beta2);
+  a.g_f32 = D.g_dtype == MAPL_F32; a.low = low; a.step = D.step; a.seed = D.seed;
+  a.stats = stats; a.step_at = step; a.lr_at = lr;
+  hipStream_t s = (hipStream_t)stream;
+  return for_tables(params, nullptr, count, [&](const OptimTable& t) {
+    LAUNCH("adamw:step", launch_adamw(t, a, s));
+    return (int)MAPL_OK;
+  });
+}
+
+extern "C" int mapl_adamw_unpack(const mapl_param* packed, const mapl_param* values, int64_t count, void* stream) {
+  return convert_states(packed, values, count, false, stream);
+}
+
+extern "C" int mapl_adamw_pack(const mapl_param* values, const mapl_param* packed, int64_t count, void* stream) {
+  return convert_states(packed, values, count, true, stream);
 }
 
 // ---------------------------------------------------------------- tracing API

@@ -21,8 +21,12 @@ AMBIENT, COORD = 0, 1
 CALL_ENCODE, CALL_DECODE, CALL_DECODE_BWD, CALL_ENCODE_BWD, CALL_STIEFEL = range(5)
 SENDER, RECEIVER = 0, 1
 XENT_FWD, XENT_BWD = 0, 1
+NORM_PRE, NORM_BRANCH, NORM_POST = 1, 2, 4
+STATES_F32, STATES_8BIT = 0, 1
 _DT = {"f32": F32, "bf16": BF16, "u8": U8, "u16": U16}
 _SPACE = {"ambient": AMBIENT, "coord": COORD}
+_GATE = {"none": 0, "sigmoid": 1, "silu": 2}
+_STATES = {"f32": STATES_F32, "8bit": STATES_8BIT}
 
 
 class MaplError(RuntimeError):
@@ -41,6 +45,24 @@ class CodecDesc(ctypes.Structure):
 class XentDesc(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int64), ("d", ctypes.c_int64), ("V", ctypes.c_int64), ("x_dtype", ctypes.c_int32),
                 ("dw_dtype", ctypes.c_int32)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("d", ctypes.c_int64), ("ld_h", ctypes.c_int64), ("ld_gate", ctypes.c_int64),
+                ("x_dtype", ctypes.c_int32), ("h_dtype", ctypes.c_int32), ("parts", ctypes.c_int32),
+                ("gate", ctypes.c_int32), ("alpha", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class Param(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("g", ctypes.c_void_p), ("p", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("e", ctypes.c_void_p), ("p16", ctypes.c_void_p),
+                ("weight_decay", ctypes.c_float), ("lr_scale", ctypes.c_float)]
+
+
+class AdamwDesc(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
+                ("g_dtype", ctypes.c_int32), ("states", ctypes.c_int32), ("step", ctypes.c_int32),
+                ("seed", ctypes.c_uint32)]
 
 
 _lib = None
@@ -69,6 +91,15 @@ _SIG = {
     "mapl_xent_bwd": [ctypes.POINTER(XentDesc)] + [_P] * 5 + [ctypes.c_float] + [_P] * 2 + [ctypes.c_int, _P,
                                                                                           ctypes.c_size_t, _P],
     "mapl_xent_workspace_bytes": [ctypes.POINTER(XentDesc), ctypes.c_int],
+    "mapl_norm_fwd": [ctypes.POINTER(NormDesc)] + [_P] * 9,
+    "mapl_norm_bwd": [ctypes.POINTER(NormDesc)] + [_P] * 14 + [ctypes.c_int, _P, ctypes.c_size_t, _P],
+    "mapl_norm_workspace_bytes": [ctypes.POINTER(NormDesc)],
+    "mapl_grad_norm": [_P, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_float, _P, _P, _P, ctypes.c_size_t,
+                       _P],
+    "mapl_grad_norm_workspace_bytes": [_P, ctypes.c_int64, ctypes.c_int32],
+    "mapl_adamw_step": [ctypes.POINTER(AdamwDesc), _P, ctypes.c_int64] + [_P] * 4,
+    "mapl_adamw_unpack": [_P, _P, ctypes.c_int64, _P],
+    "mapl_adamw_pack": [_P, _P, ctypes.c_int64, _P],
     "mapl_stiefel_step": [ctypes.c_int64] * 3 + [_P] * 3 + [ctypes.c_float, ctypes.c_float, ctypes.c_int,
                                                             ctypes.c_int, _P, ctypes.c_size_t, _P],
     "mapl_workspace_bytes": [ctypes.POINTER(CodecDesc), ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
@@ -80,7 +111,8 @@ _SIG = {
 }
 _RES = {"mapl_workspace_bytes": ctypes.c_size_t, "mapl_decode_bwd_q_workspace_bytes": ctypes.c_size_t,
         "mapl_anchor_bwd_workspace_bytes": ctypes.c_size_t, "mapl_ckpt_encode_bwd_workspace_bytes": ctypes.c_size_t,
-        "mapl_xent_workspace_bytes": ctypes.c_size_t,
+        "mapl_xent_workspace_bytes": ctypes.c_size_t, "mapl_norm_workspace_bytes": ctypes.c_size_t,
+        "mapl_grad_norm_workspace_bytes": ctypes.c_size_t,
         "mapl_last_error": ctypes.c_char_p}
 EXPORTS = tuple(_SIG)
 
@@ -302,6 +334,119 @@ def xent_bwd(D, H, W, targets, lse, weight, scale, dH, dW, accumulate_dW, ws, ws
     wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
     _check(lib().mapl_xent_bwd(ctypes.byref(D), _ptr(H), _ptr(W), _ptr(targets), _ptr(lse), _ptr(weight), float(scale),
                                _ptr(dH), _ptr(dW), int(accumulate_dW), _ptr(ws), wb, _stream(stream)))
+
+
+def norm_desc(T, d, x_dtype="bf16", h_dtype=None, branch=False, post=False, pre=True, gate="none", alpha=1.0, eps=1e-5,
+              ld_h=0, ld_gate=0):
+    """Build a mapl_norm_desc: pre (a norm in front of a block), branch (a block's output added to the
+    residual stream, with post after a norm of its own), or both; h_dtype defaults to x_dtype."""
+    parts = NORM_PRE * bool(pre) | NORM_BRANCH * bool(branch) | NORM_POST * bool(post)
+    h_dtype = x_dtype if h_dtype is None else h_dtype
+    return NormDesc(T, d, ld_h, ld_gate, _DT.get(x_dtype, x_dtype), _DT.get(h_dtype, h_dtype), parts,
+                    _GATE.get(gate, gate), alpha, eps)
+
+
+def norm_workspace_bytes(D):
+    """Bytes that norm_bwd needs."""
+    n = lib().mapl_norm_workspace_bytes(ctypes.byref(D))
+    if n == 0 and last_error():
+        raise MaplError(-2, last_error())
+    return n
+
+
+def norm_fwd(D, x, h, gate, w_post, scale, w_pre, xo, y, stream=None):
+    """xo = x + alpha scale rms(h) w_post act(gate), y = rms(xo) w_pre; what D leaves out is None."""
+    _check(lib().mapl_norm_fwd(ctypes.byref(D), _ptr(x), _ptr(h), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre),
+                               _ptr(xo), _ptr(y), _stream(stream)))
+
+
+def norm_bwd(D, dy, dxo, xo, h, gate, w_post, scale, w_pre, dx, dh, dgate, dw_post, dscale, dw_pre, accumulate_dw, ws,
+             ws_bytes=None, stream=None):
+    """Its gradient; the vectors' (any may be None) are added to with accumulate_dw."""
+    wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
+    _check(lib().mapl_norm_bwd(ctypes.byref(D), _ptr(dy), _ptr(dxo), _ptr(xo), _ptr(h), _ptr(gate), _ptr(w_post),
+                               _ptr(scale), _ptr(w_pre), _ptr(dx), _ptr(dh), _ptr(dgate), _ptr(dw_post), _ptr(dscale),
+                               _ptr(dw_pre), int(accumulate_dw), _ptr(ws), wb, _stream(stream)))
+
+
+class OptimParams:
+    """A host array of mapl_param and the tensors that it points to (kept alive with it)."""
+
+    def __init__(self, array, count, tensors):
+        self.array, self.count, self.tensors = array, count, tensors
+
+
+def optim_params(g, p=None, m=None, v=None, e=None, p16=None, weight_decay=0.0, lr_scale=1.0):
+    """The tensors of an optimizer step: sequences of equal length (e, p16 and what a call does not
+    use may be None); weight_decay and lr_scale are numbers or sequences of them."""
+    count = len(g)
+    lists = {"g": g, "p": p, "m": m, "v": v, "e": e, "p16": p16}
+    each = lambda x: list(x) if hasattr(x, "__len__") else [x] * count
+    decay, lr = each(weight_decay), each(lr_scale)
+    for name, x in list(lists.items()) + [("weight_decay", decay), ("lr_scale", lr)]:
+        if x is not None and len(x) != count:
+            raise ValueError("%s has %d entries, g %d" % (name, len(x), count))
+    a = (Param * count)()
+    for i in range(count):
+        n = g[i].numel()
+        for name, x in lists.items():
+            t = None if x is None else x[i]
+            if t is None:
+                continue
+            if not t.is_contiguous():
+                raise ValueError("%s[%d] is not contiguous" % (name, i))
+            if name == "e":
+                if t.numel() < optim_exponents(n):
+                    raise ValueError("e[%d] has %d bytes, %d needed" % (i, t.numel(), optim_exponents(n)))
+            elif t.numel() != n:
+                raise ValueError("%s[%d] has %d values, g[%d] %d" % (name, i, t.numel(), i, n))
+            setattr(a[i], name, t.data_ptr() or None)
+        a[i].n, a[i].weight_decay, a[i].lr_scale = n, decay[i], lr[i]
+    return OptimParams(a, count, lists)
+
+
+def optim_exponents(n):
+    """Exponent bytes of the 8-bit states of n values."""
+    return -(-n // 128) * 2
+
+
+def grad_norm_workspace_bytes(params, g_dtype="f32"):
+    n = lib().mapl_grad_norm_workspace_bytes(params.array, params.count, _DT.get(g_dtype, g_dtype))
+    if n == 0 and last_error():
+        raise MaplError(-2, last_error())
+    return n
+
+
+def grad_norm(params, stats, ws, step=None, grad_scale=1.0, max_norm=float("inf"), g_dtype="f32", ws_bytes=None, stream=None):
+    """stats[0]: the norm of all gradients, stats[1]: the factor that clips them; counts step up if it is finite."""
+    wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
+    _check(lib().mapl_grad_norm(params.array, params.count, _DT.get(g_dtype, g_dtype), grad_scale, max_norm, _ptr(stats),
+                                _ptr(step), _ptr(ws), wb, _stream(stream)))
+
+
+def adamw_desc(lr, beta1=0.9, beta2=0.95, eps=1e-8, g_dtype="f32", states="f32", step=0, seed=0):
+    """Build a mapl_adamw_desc (step: the number of this step, from 1, where no device step is given)."""
+    return AdamwDesc(lr, beta1, beta2, eps, _DT.get(g_dtype, g_dtype), _STATES.get(states, states), step, seed)
+
+
+def adamw_step(A, params, stats=None, step=None, lr=None, stream=None):
+    """One step over all of params; stats as grad_norm leaves it, step (int32) and lr (fp32) on the device."""
+    _check(lib().mapl_adamw_step(ctypes.byref(A), params.array, params.count, _ptr(stats), _ptr(step), _ptr(lr),
+                                 _stream(stream)))
+
+
+def adamw_unpack(packed, values, stream=None):
+    """The values of 8-bit states, as fp32 m and v."""
+    if packed.count != values.count:
+        raise ValueError("%d and %d tensors" % (packed.count, values.count))
+    _check(lib().mapl_adamw_unpack(packed.array, values.array, packed.count, _stream(stream)))
+
+
+def adamw_pack(values, packed, stream=None):
+    """fp32 m and v in 8 bits, rounded to nearest."""
+    if packed.count != values.count:
+        raise ValueError("%d and %d tensors" % (packed.count, values.count))
+    _check(lib().mapl_adamw_pack(values.array, packed.array, packed.count, _stream(stream)))
 
 
 def stiefel_step(P, d, r, U, G, M, lr, beta, lmo_steps, retract_steps, ws, ws_bytes=None, stream=None):

@@ -424,6 +424,7 @@ enum { NORM_SIGMOID = 1, NORM_SILU = 2 };               // those of MAPL_GATE_*
 struct NormArgs {
   int64_t T, ld_h, ld_g;
   int d, parts, act, x_f32, h_f32;
+  int once;  // nothing finds these rows in a cache again before others have taken their place
   float alpha, eps;
   const void *x, *h, *gate, *dy, *dxo;
   const float *w_post, *scale, *w_pre;
@@ -431,8 +432,8 @@ struct NormArgs {
   float* part;
 };
 hipError_t launch_norm_fwd(const NormArgs& g, hipStream_t s);
-// T >= 1; leaves part [norm_bwd_parts(T, d)][3][d] fp32 (dw_post, dscale, dw_pre).
-int norm_bwd_parts(int64_t T, int d);
+// T >= 1; leaves part [norm_bwd_parts(T, d, parts)][3][d] fp32 (dw_post, dscale, dw_pre).
+int norm_bwd_parts(int64_t T, int d, int parts);
 hipError_t launch_norm_bwd(const NormArgs& g, hipStream_t s);
 struct NormSums {
   float *dw_post, *dscale, *dw_pre;  // [d], null: left out
@@ -457,12 +458,13 @@ struct OptimTable {
 int64_t optim_pieces(int64_t n);
 // part[0 .. grad_norm_parts(pieces) - 1]: sums of squares (64 bits)
 int grad_norm_parts(int64_t pieces);
-hipError_t launch_grad_squares(const OptimTable& t, int g_f32, double* part, hipStream_t s);
+// once: nothing finds these lines in a cache again before others have taken their place
+hipError_t launch_grad_squares(const OptimTable& t, int g_f32, int once, double* part, hipStream_t s);
 hipError_t launch_grad_norm(const double* part, int n, float grad_scale, float max_norm, float* stats, int32_t* step,
                             hipStream_t s);
 struct AdamwArgs {
   float lr, eps, c1, c2, ln_b1, ln_b2;  // c = 1 - b, ln_b = log b
-  int g_f32, low, step;
+  int g_f32, low, step, once;
   uint32_t seed;
   const float *stats, *lr_at;
   const int32_t* step_at;

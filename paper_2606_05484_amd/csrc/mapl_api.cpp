@@ -1802,7 +1802,7 @@ struct NormLayout {
 NormLayout norm_layout(const mapl_norm_desc& D) {
   NormLayout L;
   Carve c;
-  L.part = c.take((size_t)norm_bwd_parts(D.T > 0 ? D.T : 1, (int)D.d) * 3 * D.d * 4);
+  L.part = c.take((size_t)norm_bwd_parts(D.T > 0 ? D.T : 1, (int)D.d, D.parts) * 3 * D.d * 4);
   L.total = c.off;
   return L;
 }
@@ -1854,13 +1854,18 @@ int only_with(bool on, std::initializer_list<Span> s, const char* what) {
   return MAPL_OK;
 }
 
-NormArgs norm_args(const mapl_norm_desc& D) {
+// (x and h arrays that the call reads and writes: past half of the last-level cache of 256 MiB nothing finds
+// its rows there again, and loads and stores that bypass it are faster: the forward at T = 8192,
+// d = 2048 in bf16 (168 MB) 38.8 us and 35.6, the backward at T = 8192, d = 1024 52 and 48;
+// below it they are slower: T = 2048, d = 4096 (84 MB) 18.9 and 21.0.)
+NormArgs norm_args(const mapl_norm_desc& D, int x_arrays, int h_arrays) {
   NormArgs g{};
   g.T = D.T; g.d = (int)D.d;
   g.ld_h = D.ld_h ? D.ld_h : D.d; g.ld_g = D.ld_gate ? D.ld_gate : D.d;
   g.parts = D.parts; g.act = D.gate;
   g.x_f32 = D.x_dtype == MAPL_F32; g.h_f32 = D.h_dtype == MAPL_F32;
   g.alpha = D.alpha; g.eps = D.eps;
+  g.once = D.T * D.d * (int64_t)(x_arrays * esize(D.x_dtype) + h_arrays * esize(D.h_dtype)) > ((int64_t)128 << 20);
   return g;
 }
 }  // namespace
@@ -1895,7 +1900,7 @@ extern "C" int mapl_norm_fwd(const mapl_norm_desc* desc, const void* x, const vo
   if (!st) st = check_ptrs({}, {{xo, xb, "xo"}}, {{y, yb, "y"}});
   if (st) return st;
   if (D.T == 0) return MAPL_OK;
-  NormArgs g = norm_args(D);
+  NormArgs g = norm_args(D, 1 + br, br + gated + pre);
   g.x = x; g.h = h; g.gate = gate; g.w_post = w_post; g.scale = scale; g.w_pre = w_pre;
   g.xo = xo; g.y = y;
   hipStream_t s = (hipStream_t)stream;
@@ -1936,14 +1941,14 @@ extern "C" int mapl_norm_bwd(const mapl_norm_desc* desc, const void* dy, const v
   if (!st) st = check_ptrs({}, {{dw_post, vb, "dw_post"}}, {{dscale, vb, "dscale"}, {dw_pre, vb, "dw_pre"}});
   if (!st) st = check_ptrs({}, {{dscale, vb, "dscale"}}, {{dw_pre, vb, "dw_pre"}});
   if (st) return st;
-  NormArgs g = norm_args(D);
+  NormArgs g = norm_args(D, 1 + 2 * pre, pre + 2 * br + 2 * gated);
   if (rows_overlap(dh, dgate, hb, gb, g.ld_h, g.ld_g, D.d, es)) return fail(MAPL_E_ALIAS, "output dh overlaps output dgate");
   const NormLayout L = norm_layout(D);
   if ((st = check_ws(ws, ws_bytes, L.total))) return st;
   hipStream_t s = (hipStream_t)stream;
   const NormSums o{dw_post, dscale, dw_pre};
   const bool sums = dw_post || dscale || dw_pre;
-  const int n = D.T ? norm_bwd_parts(D.T, (int)D.d) : 0;
+  const int n = D.T ? norm_bwd_parts(D.T, (int)D.d, D.parts) : 0;
   if (D.T) {
     g.x = xo; g.h = h; g.gate = gate; g.dy = dy; g.dxo = dxo;
     g.w_post = w_post; g.scale = scale; g.w_pre = w_pre;
@@ -1960,44 +1965,98 @@ extern "C" int mapl_norm_bwd(const mapl_norm_desc* desc, const void* dy, const v
 namespace {
 constexpr int64_t kMaxParams = (int64_t)1 << 20, kMaxValues = (int64_t)1 << 38;
 
-// Every array of a call with its extent, to be looked through for overlaps: an
-// output with anything, the same tensor given twice included.
+// The arrays of a call over many tensors, each with the kind it belongs to (p, g,
+// m, ...), to be looked through for overlaps: an output with anything, the same
+// tensor given twice included.  Where every kind's arrays follow each other in memory
+// and the kinds lie apart (flat arrays cut into tensors), two ends for each
+// kind tell; else all are sorted (43 tensors: 3 us against 8 on the host).
 struct Extents {
+  static constexpr int KINDS = 9;
   struct X {
     uintptr_t lo, hi;
-    bool out;
-    const char* name;
+    int kind;
     int64_t of;
   };
-  std::vector<X> all;
-  int64_t of = -1;  // the tensor whose arrays are being added
-  int st = MAPL_OK;
-  void add(const void* p, int64_t bytes, const char* name, bool out, bool need = true) {
-    if (st || bytes == 0 || (!p && !need)) return;
-    char where[32] = "";
-    if (of >= 0) snprintf(where, sizeof where, "params[%lld].", (long long)of);
-    if (!p)
-      st = fail(MAPL_E_NULL, "%s%s is NULL", where, name);
-    else if (!aligned(p, 16))
-      st = fail(MAPL_E_ALIGN, "%s%s is not 16-byte aligned", where, name);
-    else
-      all.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, out, name, of});
+  struct Kind {
+    const char* name;
+    bool out;
+    uintptr_t lo = UINTPTR_MAX, hi = 0;
+    bool in_turn = true;
+  };
+  Kind kind[KINDS];
+  int kinds = 0, st = MAPL_OK;
+  std::vector<X>* all = nullptr;  // where they are to be sorted
+  int add_kind(const char* name, bool out) {
+    if (!all) {
+      kind[kinds].name = name;
+      kind[kinds].out = out;
+    }
+    return kinds++;
   }
-  int check() {
-    if (st) return st;
-    std::sort(all.begin(), all.end(), [](const X& a, const X& b) { return a.lo < b.lo; });
+  // of: the tensor, -1 for an array that the call has once
+  void add(int k, int64_t of, const void* p, int64_t bytes, bool need = true) {
+    if (bytes == 0 || (!p && !need)) return;
+    const uintptr_t lo = (uintptr_t)p, hi = lo + (uintptr_t)bytes;
+    if (all) {
+      all->push_back({lo, hi, k, of});
+      return;
+    }
+    Kind& q = kind[k];
+    if (!p || (lo & 15)) bad(k, of, p);
+    q.in_turn = q.in_turn && lo >= q.hi;
+    if (lo < q.lo) q.lo = lo;
+    if (hi > q.hi) q.hi = hi;
+  }
+  void bad(int k, int64_t of, const void* p) {
+    char where[48] = "";
+    if (of >= 0) snprintf(where, sizeof where, "params[%lld].", (long long)of);
+    if (!st)
+      st = p ? fail(MAPL_E_ALIGN, "%s%s is not 16-byte aligned", where, kind[k].name) : fail(MAPL_E_NULL, "%s%s is NULL", where, kind[k].name);
+  }
+  bool apart() const {
+    for (int i = 0; i < kinds; ++i) {
+      if (kind[i].out && !kind[i].in_turn) return false;
+      for (int j = 0; j < i; ++j)
+        if ((kind[i].out || kind[j].out) && kind[i].lo < kind[j].hi && kind[j].lo < kind[i].hi) return false;
+    }
+    return true;
+  }
+  int sorted(std::vector<X>& v) const {
+    std::sort(v.begin(), v.end(), [](const X& a, const X& b) { return a.lo < b.lo; });
     const X *far = nullptr, *far_out = nullptr;  // those that reach furthest
-    for (const X& x : all) {
-      const X* y = x.out && far && far->hi > x.lo ? far : far_out && far_out->hi > x.lo ? far_out : nullptr;
-      if (y)
-        return fail(MAPL_E_ALIAS, "%s (tensor %lld) overlaps %s (tensor %lld)", x.out ? x.name : y->name,
-                    (long long)(x.out ? x.of : y->of), x.out ? y->name : x.name, (long long)(x.out ? y->of : x.of));
+    for (const X& x : v) {
+      const bool out = kind[x.kind].out;
+      const X* y = out && far && far->hi > x.lo ? far : far_out && far_out->hi > x.lo ? far_out : nullptr;
+      if (y) {
+        const X &a = out ? x : *y, &b = out ? *y : x;
+        return fail(MAPL_E_ALIAS, "output %s (tensor %lld) overlaps %s (tensor %lld)", kind[a.kind].name, (long long)a.of,
+                    kind[b.kind].name, (long long)b.of);
+      }
       if (!far || x.hi > far->hi) far = &x;
-      if (x.out && (!far_out || x.hi > far_out->hi)) far_out = &x;
+      if (out && (!far_out || x.hi > far_out->hi)) far_out = &x;
     }
     return MAPL_OK;
   }
 };
+
+// visit(extents) adds every array of the call: once for its pointer and its kind's
+// ends, and once more where that leaves an overlap possible.
+template <typename F>
+int check_extents(int64_t count, F&& visit) {
+  try {
+    Extents x;
+    visit(x);
+    if (x.st || x.apart()) return x.st;
+    std::vector<Extents::X> v;
+    v.reserve((size_t)count * 6 + 4);
+    x.all = &v;
+    x.kinds = 0;
+    visit(x);
+    return x.sorted(v);
+  } catch (const std::bad_alloc&) {
+    return fail(MAPL_E_UNSUPPORTED, "no host memory to check %lld tensors", (long long)count);
+  }
+}
 
 int check_params(const mapl_param* params, int64_t count) {
   if (count < 0 || count > kMaxParams) return fail(MAPL_E_SHAPE, "count=%lld: need 0 <= count <= 2^20", (long long)count);
@@ -2037,6 +2096,17 @@ int for_tables(const mapl_param* params, const mapl_param* values, int64_t count
   return MAPL_OK;
 }
 
+// Whether a call's arrays, `bytes` a value, are more than the last-level cache (256 MiB) will keep
+// until the next call reads them: then loads and stores that bypass it are
+// faster (adamw_step, 266 M values in fp32: 1396 us, bypassing it 1302; 10 M values, 312 MB, after
+// other work: 65.5 and 57.1; in 8 bits, 167 MB, 46.4 and 42.4), else they can be slower (10 M values in fp32 again and again, with nothing
+// between: 46.9 and 53.5).
+int streams(const mapl_param* params, int64_t count, int64_t bytes) {
+  int64_t n = 0;
+  for (int64_t i = 0; i < count; ++i) n += params[i].n;
+  return n > ((int64_t)128 << 20) / bytes;
+}
+
 int64_t grad_parts(const mapl_param* params, int64_t count) {
   int64_t n = 0;
   for_tables(params, nullptr, count, [&](const OptimTable& t) {
@@ -2051,23 +2121,23 @@ int convert_states(const mapl_param* packed, const mapl_param* values, int64_t c
   int st = check_params(packed, count);
   if (!st) st = check_params(values, count);
   if (st) return st;
-  try {
-    Extents x;
+  for (int64_t i = 0; i < count; ++i)
+    if (packed[i].n != values[i].n)
+      return fail(MAPL_E_SHAPE, "tensor %lld has %lld values packed and %lld unpacked", (long long)i, (long long)packed[i].n,
+                  (long long)values[i].n);
+  st = check_extents(count, [&](Extents& x) {
+    const int m = x.add_kind("m", pack), v = x.add_kind("v", pack), e = x.add_kind("e", pack);
+    const int m32 = x.add_kind("m (fp32)", !pack), v32 = x.add_kind("v (fp32)", !pack);
     for (int64_t i = 0; i < count; ++i) {
       const mapl_param &q = packed[i], &u = values[i];
-      if (q.n != u.n)
-        return fail(MAPL_E_SHAPE, "tensor %lld has %lld values packed and %lld unpacked", (long long)i, (long long)q.n, (long long)u.n);
-      x.of = i;
-      x.add(q.m, q.n, "m", pack);
-      x.add(q.v, q.n, "v", pack);
-      x.add(q.e, (q.n + 127) / 128 * 2, "e", pack);
-      x.add(u.m, 4 * q.n, "m (fp32)", !pack);
-      x.add(u.v, 4 * q.n, "v (fp32)", !pack);
+      x.add(m, i, q.m, q.n);
+      x.add(v, i, q.v, q.n);
+      x.add(e, i, q.e, (q.n + 127) / 128 * 2);
+      x.add(m32, i, u.m, 4 * q.n);
+      x.add(v32, i, u.v, 4 * q.n);
     }
-    if ((st = x.check())) return st;
-  } catch (const std::bad_alloc&) {
-    return fail(MAPL_E_UNSUPPORTED, "no host memory to check %lld tensors", (long long)count);
-  }
+  });
+  if (st) return st;
   hipStream_t s = (hipStream_t)stream;
   return for_tables(packed, values, count, [&](const OptimTable& t) {
     if (pack)
@@ -2096,24 +2166,22 @@ extern "C" int mapl_grad_norm(const mapl_param* params, int64_t count, int32_t g
   const size_t need = (size_t)rup(8 * grad_parts(params, count), 256) + 256;
   if (!stats) return fail(MAPL_E_NULL, "stats is NULL");
   if ((st = check_ws(ws, ws_bytes, need))) return st;
-  try {
-    Extents x;
-    x.add(stats, 8, "stats", true);
-    x.add(step, 4, "step", true, false);
-    x.add(ws, (int64_t)ws_bytes, "workspace", true);
-    for (int64_t i = 0; i < count; ++i) {
-      x.of = i;
-      x.add(params[i].g, params[i].n * (int64_t)esize(g_dtype), "g", false);
-    }
-    if ((st = x.check())) return st;
-  } catch (const std::bad_alloc&) {
-    return fail(MAPL_E_UNSUPPORTED, "no host memory to check %lld tensors", (long long)count);
-  }
+  st = check_extents(count, [&](Extents& x) {
+    const int a = x.add_kind("stats", true), b = x.add_kind("step", true), w = x.add_kind("workspace", true);
+    const int g = x.add_kind("g", false);
+    x.add(a, -1, stats, 8);
+    x.add(b, -1, step, 4, false);
+    x.add(w, -1, ws, (int64_t)ws_bytes);
+    const int64_t es = (int64_t)esize(g_dtype);
+    for (int64_t i = 0; i < count; ++i) x.add(g, i, params[i].g, params[i].n * es);
+  });
+  if (st) return st;
   hipStream_t s = (hipStream_t)stream;
   double* part = (double*)ws;
   int64_t n = 0;
+  const int once = streams(params, count, (int64_t)esize(g_dtype));
   st = for_tables(params, nullptr, count, [&](const OptimTable& t) {
-    LAUNCH("grad_norm:squares", launch_grad_squares(t, g_dtype == MAPL_F32, part + n, s));
+    LAUNCH("grad_norm:squares", launch_grad_squares(t, g_dtype == MAPL_F32, once, part + n, s));
     n += grad_norm_parts(t.first[t.count]);
     return (int)MAPL_OK;
   });
@@ -2137,32 +2205,33 @@ extern "C" int mapl_adamw_step(const mapl_adamw_desc* desc, const mapl_param* pa
   if (!lr && !std::isfinite(D.lr)) return fail(MAPL_E_SHAPE, "lr is not finite");
   if (!step && D.step < 1) return fail(MAPL_E_SHAPE, "step=%d: the first step is 1", D.step);
   const bool low = D.states == MAPL_STATES_8BIT;
-  try {
-    Extents x;
-    x.add(stats, 8, "stats", false, false);
-    x.add(step, 4, "step", false, false);
-    x.add(lr, 4, "lr", false, false);
+  for (int64_t i = 0; i < count; ++i)
+    if (!std::isfinite(params[i].weight_decay) || !std::isfinite(params[i].lr_scale))
+      return fail(MAPL_E_SHAPE, "params[%lld]: weight_decay or lr_scale is not finite", (long long)i);
+  st = check_extents(count, [&](Extents& x) {
+    const int a = x.add_kind("stats", false), b = x.add_kind("step", false), c = x.add_kind("lr", false);
+    const int g = x.add_kind("g", false), p = x.add_kind("p", true), m = x.add_kind("m", true), v = x.add_kind("v", true);
+    const int e = x.add_kind("e", true), p16 = x.add_kind("p16", true);
+    x.add(a, -1, stats, 8, false);
+    x.add(b, -1, step, 4, false);
+    x.add(c, -1, lr, 4, false);
+    const int64_t ge = (int64_t)esize(D.g_dtype), se = low ? 1 : 4;
     for (int64_t i = 0; i < count; ++i) {
-      const mapl_param& p = params[i];
-      if (!std::isfinite(p.weight_decay) || !std::isfinite(p.lr_scale))
-        return fail(MAPL_E_SHAPE, "params[%lld]: weight_decay or lr_scale is not finite", (long long)i);
-      x.of = i;
-      x.add(p.g, p.n * (int64_t)esize(D.g_dtype), "g", false);
-      x.add(p.p, 4 * p.n, "p", true);
-      x.add(p.m, low ? p.n : 4 * p.n, "m", true);
-      x.add(p.v, low ? p.n : 4 * p.n, "v", true);
-      if (low) x.add(p.e, (p.n + 127) / 128 * 2, "e", true);
-      x.add(p.p16, 2 * p.n, "p16", true, false);
+      const mapl_param& q = params[i];
+      x.add(g, i, q.g, q.n * ge);
+      x.add(p, i, q.p, 4 * q.n);
+      x.add(m, i, q.m, se * q.n);
+      x.add(v, i, q.v, se * q.n);
+      if (low) x.add(e, i, q.e, (q.n + 127) / 128 * 2);
+      x.add(p16, i, q.p16, 2 * q.n, false);
     }
-    if ((st = x.check())) return st;
-  } catch (const std::bad_alloc&) {
-    return fail(MAPL_E_UNSUPPORTED, "no host memory to check %lld tensors", (long long)count);
-  }
+  });
+  if (st) return st;
   AdamwArgs a{};
   a.lr = D.lr; a.eps = D.eps;
   a.c1 = (float)(1.0 - (double)D.beta1); a.c2 = (float)(1.0 - (double)D.beta2);
   a.ln_b1 = (float)std::log((double)D.beta1); a.ln_b2 = (float)std::log((double)D.beta2);
-  a.g_f32 = D.g_dtype == MAPL_F32; a.low = low; a.step = D.step; a.seed = D.seed;
+  a.g_f32 = D.g_dtype == MAPL_F32; a.low = low; a.once = streams(params, count, (low ? 12 : 24) + (int64_t)esize(D.g_dtype)); a.step = D.step; a.seed = D.seed;
   a.stats = stats; a.step_at = step; a.lr_at = lr;
   hipStream_t s = (hipStream_t)stream;
   return for_tables(params, nullptr, count, [&](const OptimTable& t) {

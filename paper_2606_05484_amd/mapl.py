@@ -8,6 +8,7 @@ MaplError when the library is missing or a call fails.
 """
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmapl.so")
@@ -386,22 +387,27 @@ def optim_params(g, p=None, m=None, v=None, e=None, p16=None, weight_decay=0.0, 
     for name, x in list(lists.items()) + [("weight_decay", decay), ("lr_scale", lr)]:
         if x is not None and len(x) != count:
             raise ValueError("%s has %d entries, g %d" % (name, len(x), count))
-    a = (Param * count)()
-    for i in range(count):
-        n = g[i].numel()
-        for name, x in lists.items():
-            t = None if x is None else x[i]
+    sizes = [t.numel() for t in g]
+    where = {}
+    for name, x in lists.items():
+        if x is None:
+            where[name] = [0] * count
+            continue
+        for i, t in enumerate(x):
             if t is None:
                 continue
             if not t.is_contiguous():
                 raise ValueError("%s[%d] is not contiguous" % (name, i))
             if name == "e":
-                if t.numel() < optim_exponents(n):
-                    raise ValueError("e[%d] has %d bytes, %d needed" % (i, t.numel(), optim_exponents(n)))
-            elif t.numel() != n:
-                raise ValueError("%s[%d] has %d values, g[%d] %d" % (name, i, t.numel(), i, n))
-            setattr(a[i], name, t.data_ptr() or None)
-        a[i].n, a[i].weight_decay, a[i].lr_scale = n, decay[i], lr[i]
+                if t.numel() < optim_exponents(sizes[i]):
+                    raise ValueError("e[%d] has %d bytes, %d needed" % (i, t.numel(), optim_exponents(sizes[i])))
+            elif t.numel() != sizes[i]:
+                raise ValueError("%s[%d] has %d values, g[%d] %d" % (name, i, t.numel(), i, sizes[i]))
+        where[name] = [0 if t is None else t.data_ptr() for t in x]
+    a = (Param * count)()
+    one = struct.Struct("=q6Q2f")  # Param's layout
+    for i, row in enumerate(zip(sizes, *(where[name] for name, _ in Param._fields_[1:7]), decay, lr)):
+        one.pack_into(a, i * one.size, *row)
     return OptimParams(a, count, lists)
 
 

@@ -356,7 +356,8 @@ size_t mapl_xent_workspace_bytes(const mapl_xent_desc* desc, int call);
  *   w_post, scale, w_pre [d] fp32, each may be NULL: ones
  *   1e-30 <= eps <= 1; alpha finite
  * Everything in between is fp32; xo is rounded to its type before y is made of it.
- * Rows of any finite size give finite results (their squares may overflow).
+ * Rows of any finite size have finite results: their squares may overflow.  (The backward's
+ * products dy w_pre xo and dn w_post h, and their sums over a row, may not.)
  * mapl_norm_bwd, from the gradients dy of y (with MAPL_NORM_PRE) and dxo of xo (NULL: zeros;
  * needed without MAPL_NORM_PRE); xo is what the forward wrote (x without a branch; not
  * read without MAPL_NORM_PRE):
@@ -386,7 +387,7 @@ size_t mapl_norm_workspace_bytes(const mapl_norm_desc* desc);
  * is neither a projector nor its other optimizer's).  `params` is a HOST array of
  * `count` tensors (0 <= count <= 2^20), read during the call; its pointers are device
  * pointers, and each call says which of them it uses.
- *   n values, 0 <= n <= 2^38; g [n] of g_dtype (MAPL_BF16 or MAPL_F32); p [n] fp32
+ *   n values, 0 <= n <= 2^34; g [n] of g_dtype (MAPL_BF16 or MAPL_F32); p [n] fp32
  *   m, v   states: MAPL_STATES_F32 fp32 [n] each; MAPL_STATES_8BIT one byte a value
  *   e      8 bits: [ceil(n/128)][2] exponent bytes (m's, then sqrt(v)'s); else not used
  *   p16    [n] bf16, may be NULL: p's new values rounded (what the next forward reads)

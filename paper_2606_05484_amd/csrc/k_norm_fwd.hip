@@ -117,8 +117,23 @@ hipError_t run(const NormArgs& g, hipStream_t s) {
     f = g.act == 0 ? k_norm_fwd<X, H, LANES, NV, true, false, 0, ONCE>
         : g.act == NORM_SILU ? k_norm_fwd<X, H, LANES, NV, true, false, NORM_SILU, ONCE>
                              : k_norm_fwd<X, H, LANES, NV, true, false, NORM_SIGMOID, ONCE>;
-  hipLaunchKernelGGL(f, dim3((unsigned)((g.T + ROWS - 1) / ROWS)), dim3(THREADS), 0, s, g);
-  return hipGetLastError();
+  // (a launch holds fewer than 2^32 threads)
+  constexpr int64_t MOST = (int64_t)1 << 21;
+  for (int64_t t = 0; t < g.T; t += MOST * ROWS) {
+    NormArgs a = g;
+    a.T = g.T - t < MOST * ROWS ? g.T - t : MOST * ROWS;
+    a.x = (const X*)g.x + t * g.d;
+    if (br) {
+      a.h = (const H*)g.h + t * g.ld_h;
+      a.xo = (X*)g.xo + t * g.d;
+      if (g.act) a.gate = (const H*)g.gate + t * g.ld_g;
+    }
+    if (pre) a.y = (H*)g.y + t * g.d;
+    hipLaunchKernelGGL(f, dim3((unsigned)((a.T + ROWS - 1) / ROWS)), dim3(THREADS), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename X, typename H, bool ONCE>

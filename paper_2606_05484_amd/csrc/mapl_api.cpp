@@ -1963,7 +1963,7 @@ extern "C" int mapl_norm_bwd(const mapl_norm_desc* desc, const void* dy, const v
 
 // ------------------------------------------------------------- optimizer step
 namespace {
-constexpr int64_t kMaxParams = (int64_t)1 << 20, kMaxValues = (int64_t)1 << 38;
+constexpr int64_t kMaxParams = (int64_t)1 << 20, kMaxValues = (int64_t)1 << 34;
 
 // The arrays of a call over many tensors, each with the kind it belongs to (p, g,
 // m, ...), to be looked through for overlaps: an output with anything, the same
@@ -2063,7 +2063,7 @@ int check_params(const mapl_param* params, int64_t count) {
   if (!params && count > 0) return fail(MAPL_E_NULL, "params is NULL");
   for (int64_t i = 0; i < count; ++i) {
     if (params[i].n < 0 || params[i].n > kMaxValues)
-      return fail(MAPL_E_SHAPE, "params[%lld].n=%lld: need 0 <= n <= 2^38", (long long)i, (long long)params[i].n);
+      return fail(MAPL_E_SHAPE, "params[%lld].n=%lld: need 0 <= n <= 2^34", (long long)i, (long long)params[i].n);
   }
   return MAPL_OK;
 }
@@ -2083,7 +2083,7 @@ int for_tables(const mapl_param* params, const mapl_param* values, int64_t count
     t.first[0] = 0;
     for (; t.count < OPTIM_TENSORS && i < count; ++i) {
       const mapl_param& p = params[i];
-      if (t.count && t.first[t.count] + optim_pieces(p.n) > ((int64_t)1 << 30)) break;
+      if (t.count && t.first[t.count] + optim_pieces(p.n) > ((int64_t)1 << 22)) break;  // (fewer than 2^32 threads a launch)
       t.t[t.count] = {p.p, p.g, p.m, p.v, p.e, (bf16_t*)p.p16, p.n, p.weight_decay, p.lr_scale};
       if (values) t.t[t.count].p = (float*)values[i].m, t.t[t.count].g = values[i].v;
       t.first[t.count + 1] = t.first[t.count] + (uint32_t)optim_pieces(p.n);

@@ -298,6 +298,37 @@ def test_against_differences():
         assert abs((up - down) / (2 * step) / float(grad.norm()) - 1) < 5e-3, name
 
 
+@pytest.mark.parametrize("T,d,x,h,kw", [
+    (33000, 256, "bf16", "bf16", {}), (9000, 1024, "f32", "bf16", dict(gate="silu")), (8200, 2048, "bf16", "bf16", dict(halves=True)),
+    (3001, 8192, "bf16", "bf16", dict(gate="none")), (2001, 16384, "bf16", "bf16", {}), (17001, 2048, "f32", "f32", dict(branch=False, post=False, gate="none")),
+    (4100, 4096, "f32", "f32", dict(post=False)), (70001, 512, "bf16", "bf16", dict(pre=False, gate="silu"))])
+def test_calls_past_the_caches(T, d, x, h, kw):
+    """More than 128 MiB of rows: the variants whose loads and stores bypass the last-level cache."""
+    print("norm large", T, d, x, h, kw, flush=True)
+    c = Case(T, d, x, h, **kw)
+    c.fwd()
+    c.bwd()
+    torch.cuda.synchronize()
+    c.check()
+
+
+@pytest.mark.parametrize("T,d", [((1 << 21) + 3, 1088), ((1 << 23) + 5, 512)])
+def test_more_rows_than_a_launch_takes(T, d):
+    D = mapl.norm_desc(T, d)
+    x = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+    y = torch.full((T, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rows = [0, 1, (1 << 21) - 1, 1 << 21, T - 2, T - 1]
+    few = torch.randn(len(rows), d, generator=g, device="cuda").to(torch.bfloat16)
+    x[rows] = few
+    mapl.norm_fwd(D, x, None, None, None, None, None, None, y)
+    torch.cuda.synchronize()
+    ref = sh.norm_y(few, None, 1e-5)
+    within(y[rows], ref, sh.norm_fwd_errors(few, ref, ref.abs(), ref, torch.bfloat16)[1], "y")
+    y[rows] = 0.0
+    assert not bool(y.any())
+
+
 def test_past_two_gib():
     """Offsets past 2^32 bytes and 2^31 values."""
     T, d = 131080, 16384

@@ -312,6 +312,48 @@ def test_on_another_stream():
     assert all(torch.equal(x, y) for x, y in zip(a.everything(), b.everything()))
 
 
+@pytest.mark.parametrize("low,n", [(False, 6000001), (True, 11000003)], ids=["f32", "8bit"])
+def test_calls_past_the_caches(low, n):
+    """More than 128 MiB: the variants whose loads and stores bypass the last-level cache."""
+    s = Stage([4097, n, 12], "bf16", low)
+    want = s.expected(3, 1)
+    mapl.adamw_step(s.desc(3, 1), s.params)
+    torch.cuda.synchronize()
+    s.check(want)
+    G = grads([40000001, 5], "f32")
+    P = mapl.optim_params(G)
+    stats = torch.zeros(2, device="cuda")
+    mapl.grad_norm(P, stats, mapl.workspace(mapl.grad_norm_workspace_bytes(P)))
+    norm = math.sqrt(sum(float(g.double().square().sum()) for g in G))
+    assert abs(float(stats[0]) / norm - 1) <= 1.01 * sh.U24
+
+
+@pytest.mark.parametrize("low", [False, True], ids=["f32", "8bit"])
+def test_tensors_between_each_other(low):
+    """All arrays of all tensors out of one buffer, tensor after tensor: legal, and nothing is lost."""
+    sizes = [1000, 5, 4096, 70001]
+    a, b = Stage(sizes, low=low), Stage(sizes, low=low)
+    buf = torch.zeros(1 << 22, dtype=torch.uint8, device="cuda")
+    at = 0
+
+    def move(t):
+        nonlocal at
+        at = -(-at // 16) * 16
+        new = buf[at:at + t.numel() * t.element_size()].view(t.dtype)
+        at += t.numel() * t.element_size()
+        return new.copy_(t.reshape(-1))
+
+    for i in range(len(sizes)):
+        for x in (b.G, b.P, b.m, b.v, b.e or [None] * 9, b.p16):
+            if x[i] is not None:
+                x[i] = move(x[i])
+    P = mapl.optim_params(b.G, b.P, b.m, b.v, b.e, b.p16, b.decay, b.lrs)
+    mapl.adamw_step(a.desc(7), a.params)
+    mapl.adamw_step(b.desc(7), P)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x.view(-1), y.view(-1)) for x, y in zip(a.everything(), b.everything()))
+
+
 def test_the_second_moment_in_8_bits_follows_the_gradients():
     """1000 steps of b2 = 0.99 from four times the right v: the mean over 8192 values ends at the
     gradients' variance.  A value is off by 0.13 of s at most (its spread), so the mean of v by

@@ -152,7 +152,7 @@ def test_gradient_norm_refusals(kw, status):
     assert mapl.last_error() != ""
 
 
-@pytest.mark.parametrize("kw,status", [(dict(g=None), -1), (dict(g=P[0] + 8), -5), (dict(n=-1), -2), (dict(n=(1 << 38) + 1), -2)])
+@pytest.mark.parametrize("kw,status", [(dict(g=None), -1), (dict(g=P[0] + 8), -5), (dict(n=-1), -2), (dict(n=(1 << 34) + 1), -2)])
 def test_gradient_norm_refuses_a_tensor(kw, status):
     assert norm(params(**kw)) == status
     assert mapl.last_error() != ""
@@ -254,6 +254,27 @@ def test_the_binding_refuses_lists_that_do_not_match():
         mapl.adamw_unpack(a, mapl.optim_params([]))
     with pytest.raises(ValueError):
         mapl.adamw_pack(mapl.optim_params([]), a)
+
+
+def test_the_binding_refuses_types_that_a_call_does_not_take():
+    import torch
+    z = lambda dt: torch.zeros(300, dtype=dt)
+    f32, bf, u8 = torch.float32, torch.bfloat16, torch.uint8
+    with pytest.raises(ValueError):
+        mapl.optim_params([z(f32), z(bf)])
+    good = dict(g=[z(f32)], p=[z(f32)], m=[z(u8)], v=[z(u8)], e=[z(u8)], p16=[z(bf)])
+    step = lambda a, **kw: mapl.adamw_step(mapl.adamw_desc(1e-3, step=1, **kw), a, stream=0)
+    for name, dt in (("g", bf), ("p", bf), ("m", f32), ("v", f32), ("e", f32), ("p16", f32)):
+        with pytest.raises(ValueError):
+            step(mapl.optim_params(**dict(good, **{name: [z(dt)]})), states="8bit")
+    with pytest.raises(ValueError):
+        step(mapl.optim_params(**good))  # fp32 states asked for
+    with pytest.raises(ValueError):
+        mapl.grad_norm(mapl.optim_params([z(f32)]), None, None, g_dtype="bf16")
+    with pytest.raises(ValueError):
+        mapl.adamw_unpack(mapl.optim_params(**good), mapl.optim_params([z(f32)], m=[z(u8)], v=[z(u8)]))
+    with pytest.raises(ValueError):
+        mapl.adamw_pack(mapl.optim_params([z(f32)], m=[z(f32)], v=[z(f32)]), mapl.optim_params([z(f32)], m=[z(f32)], v=[z(f32)], e=[z(u8)]))
 
 
 def test_descriptor_layouts_match_the_header():

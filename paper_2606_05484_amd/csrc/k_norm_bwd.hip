@@ -8,7 +8,10 @@
 // keeps nothing for it.  Sums and everything in between are fp32.
 //
 // Bound by HBM (16 bytes a value where everything is bf16) and nearly as much by the vector
-// unit: about 45 operations a value.
+// unit, about 45 operations a value: T = 32768, d = 2048 with a gated branch 200 us, 5.4 TB/s, and 4.5
+// for the parts' sum; with 110 operations a value (a gate's kind decided for each, IEEE divisions, the
+// vectors loaded for every row) 237.  The next row's loads issued ahead cost a third of
+// the occupancy and gained nothing (224).
 #include "norm_rows.hpp"
 
 namespace mapl {
@@ -19,9 +22,9 @@ namespace {
 // THREADS / LANES rows at a time, adds its rows' shares of the vectors' gradients in
 // registers and then over its groups of lanes in LDS, and leaves them in
 // part[workgroup][3][d] (dw_post, ds, dw_pre).
-template <typename X, typename H, int LANES, int NV, bool BRANCH, bool PRE, int GATE, bool ONCE>
-__global__ __launch_bounds__(norm_threads(LANES)) void k_norm_bwd(const NormArgs g) {
-  constexpr int THREADS = norm_threads(LANES), ROWS = THREADS / LANES;
+template <typename X, typename H, int LANES, int NV, int THREADS, bool BRANCH, bool PRE, int GATE, bool ONCE>
+__global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormArgs g) {
+  constexpr int ROWS = THREADS / LANES;
   constexpr bool SPLIT = sizeof(X) == 4, FINE = sizeof(H) == 4;
   constexpr int NS = (BRANCH ? 2 : 0) + (PRE ? 1 : 0), S0 = BRANCH ? 0 : 2;  // sums: dw_post, ds, dw_pre
   __shared__ float lds[sums_floats(LANES, ROWS)];
@@ -262,44 +265,54 @@ __global__ __launch_bounds__(1024) void k_norm_sum(const float* __restrict__ par
   }
 }
 
-template <typename X, typename H, int LANES, int NV, bool ONCE>
+template <typename X, typename H, int LANES, int NV, int THREADS, bool ONCE>
 hipError_t run(const NormArgs& g, hipStream_t s) {
-  constexpr int THREADS = norm_threads(LANES);
   const bool br = g.parts & NORM_BRANCH, pre = g.parts & NORM_PRE;
-  void (*f)(NormArgs) = k_norm_bwd<X, H, LANES, NV, false, true, 0, ONCE>;
+  void (*f)(NormArgs) = k_norm_bwd<X, H, LANES, NV, THREADS, false, true, 0, ONCE>;
   if (br && pre)
-    f = g.act == 0 ? k_norm_bwd<X, H, LANES, NV, true, true, 0, ONCE>
-        : g.act == NORM_SILU ? k_norm_bwd<X, H, LANES, NV, true, true, NORM_SILU, ONCE>
-                             : k_norm_bwd<X, H, LANES, NV, true, true, NORM_SIGMOID, ONCE>;
+    f = g.act == 0 ? k_norm_bwd<X, H, LANES, NV, THREADS, true, true, 0, ONCE>
+        : g.act == NORM_SILU ? k_norm_bwd<X, H, LANES, NV, THREADS, true, true, NORM_SILU, ONCE>
+                             : k_norm_bwd<X, H, LANES, NV, THREADS, true, true, NORM_SIGMOID, ONCE>;
   else if (br)
-    f = g.act == 0 ? k_norm_bwd<X, H, LANES, NV, true, false, 0, ONCE>
-        : g.act == NORM_SILU ? k_norm_bwd<X, H, LANES, NV, true, false, NORM_SILU, ONCE>
-                             : k_norm_bwd<X, H, LANES, NV, true, false, NORM_SIGMOID, ONCE>;
+    f = g.act == 0 ? k_norm_bwd<X, H, LANES, NV, THREADS, true, false, 0, ONCE>
+        : g.act == NORM_SILU ? k_norm_bwd<X, H, LANES, NV, THREADS, true, false, NORM_SILU, ONCE>
+                             : k_norm_bwd<X, H, LANES, NV, THREADS, true, false, NORM_SIGMOID, ONCE>;
   hipLaunchKernelGGL(f, dim3(norm_bwd_parts(g.T, g.d, g.parts)), dim3(THREADS), 0, s, g);
   return hipGetLastError();
 }
 
+// Some thousand rows of this width: workgroups of twice as many, so that more are under way at once
+// with no more parts to sum.  d = 1024, us with and without: T = 1021 12.4, 13.1; T = 3000 18.5,
+// 20.6; d = 2048: T = 1024 15.4, 16.2; T = 1500 18.6, 21.0.  (Fewer leave CUs idle: T = 64 10.1, 9.6.)
+bool wide(int64_t T, int d) {
+  const int rows = d <= 1024 ? 2 : 1;
+  return d > 512 && d <= 2048 && T > 256 * rows && T <= 2048 * rows;
+}
+
 template <typename X, typename H, bool ONCE>
 hipError_t pick(const NormArgs& g, hipStream_t s) {
-  if (g.d <= 128) return run<X, H, 16, 1, ONCE>(g, s);
-  if (g.d <= 256) return run<X, H, 32, 1, ONCE>(g, s);
-  if (g.d <= 512) return run<X, H, 64, 1, ONCE>(g, s);
-  if (g.d <= 1024) return run<X, H, 128, 1, ONCE>(g, s);
-  if (g.d <= 2048) return run<X, H, 256, 1, ONCE>(g, s);
-  if (g.d <= 4096) return run<X, H, 256, 2, ONCE>(g, s);
-  if (g.d <= 8192) return run<X, H, 512, 2, ONCE>(g, s);
-  return run<X, H, 1024, 2, ONCE>(g, s);
+  if constexpr (!ONCE) {
+    if (wide(g.T, g.d)) return g.d <= 1024 ? run<X, H, 128, 1, 512, false>(g, s) : run<X, H, 256, 1, 512, false>(g, s);
+  }
+  if (g.d <= 128) return run<X, H, 16, 1, 256, ONCE>(g, s);
+  if (g.d <= 256) return run<X, H, 32, 1, 256, ONCE>(g, s);
+  if (g.d <= 512) return run<X, H, 64, 1, 256, ONCE>(g, s);
+  if (g.d <= 1024) return run<X, H, 128, 1, 256, ONCE>(g, s);
+  if (g.d <= 2048) return run<X, H, 256, 1, 256, ONCE>(g, s);
+  if (g.d <= 4096) return run<X, H, 256, 2, 256, ONCE>(g, s);
+  if (g.d <= 8192) return run<X, H, 512, 2, 512, ONCE>(g, s);
+  return run<X, H, 1024, 2, 1024, ONCE>(g, s);
 }
 
 }  // namespace
 
 // Workgroups: two a CU (three where y is all there is, which takes fewer registers; one past
-// 4096 values, as many as fit), but one where each would see less than four rows in turn:
-// each leaves 3 d sums to be read again.  In us with 256, 512 and 768, T = 32768 and d = 2048
-// in bf16: with a gated branch 289, 205, 211; y alone 162, 98, 93; T = 1021, d = 1024 13.0, 14.1; T = 2048,
+// 4096 values, as many as fit), but one where each would see less than four rows in turn,
+// since each leaves 3 d sums to be read again.  In us with 256, 512 and 768, T = 32768 and d = 2048
+// in bf16: with a gated branch 289, 205, 211; y alone 162, 98, 93; T = 1021, d = 1024 13.0, 14.1, 14.1; T = 2048,
 // d = 8192 72.6, 81.6; T = 1024, d = 16384 171, 200.
 int norm_bwd_parts(int64_t T, int d, int parts) {
-  const int rows = d <= 128 ? 16 : d <= 256 ? 8 : d <= 512 ? 4 : d <= 1024 ? 2 : 1;
+  const int rows = (d <= 128 ? 16 : d <= 256 ? 8 : d <= 512 ? 4 : d <= 1024 ? 2 : 1) * (wide(T, d) ? 2 : 1);
   const int64_t n = (T + rows - 1) / rows;
   const int most = d > 4096 ? 256 : parts == NORM_PRE ? 768 : 512;
   const int64_t w = n / 4 > 256 ? n / 4 : 256;

@@ -1854,10 +1854,12 @@ int only_with(bool on, std::initializer_list<Span> s, const char* what) {
   return MAPL_OK;
 }
 
-// (x and h arrays that the call reads and writes: past half of the last-level cache of 256 MiB nothing finds
-// its rows there again, and loads and stores that bypass it are faster: the forward at T = 8192,
-// d = 2048 in bf16 (168 MB) 38.8 us and 35.6, the backward at T = 8192, d = 1024 52 and 48;
-// below it they are slower: T = 2048, d = 4096 (84 MB) 18.9 and 21.0.)
+// x_arrays and h_arrays: those of x's and of h's type that the call reads and writes.  Past half of the
+// last-level cache (256 MiB) nothing finds their rows there again, and loads and stores that
+// bypass it are faster: d = 1024 in bf16, three sets of arrays in turn, us with and without: forward T =
+// 16000 (164 MB) 31.0, 33.6, T = 8000 (82 MB) 17.0, 14.0; backward T = 12000 (197 MB) 48.5, 50.5,
+// T = 5000 (82 MB) 26.8, 25.2.  (One set again and again, whose rows the cache still has: T =
+// 16000 29.8, 25.0 and 58.8, 55.4.)
 NormArgs norm_args(const mapl_norm_desc& D, int x_arrays, int h_arrays) {
   NormArgs g{};
   g.T = D.T; g.d = (int)D.d;

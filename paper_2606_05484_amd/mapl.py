@@ -150,6 +150,11 @@ def _ptr(x):
     return x.data_ptr()
 
 
+def _ptrs(*xs):
+    """_ptr of several, without a Python call for each (0.04 to 0.15 us instead of 0.2 to 0.4)."""
+    return [x if x is None or isinstance(x, int) else x.data_ptr() for x in xs]
+
+
 _current = None  # torch's current raw stream, a function (torch is imported with the first use)
 
 
@@ -357,30 +362,33 @@ def norm_workspace_bytes(D):
 
 def norm_fwd(D, x, h, gate, w_post, scale, w_pre, xo, y, stream=None):
     """xo = x + alpha scale rms(h) w_post act(gate), y = rms(xo) w_pre; what D leaves out is None."""
-    _check(lib().mapl_norm_fwd(ctypes.byref(D), _ptr(x), _ptr(h), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre),
-                               _ptr(xo), _ptr(y), _stream(stream)))
+    _check(lib().mapl_norm_fwd(ctypes.byref(D), *_ptrs(x, h, gate, w_post, scale, w_pre, xo, y), _stream(stream)))
 
 
 def norm_bwd(D, dy, dxo, xo, h, gate, w_post, scale, w_pre, dx, dh, dgate, dw_post, dscale, dw_pre, accumulate_dw, ws,
              ws_bytes=None, stream=None):
     """Its gradient; the vectors' (any may be None) are added to with accumulate_dw."""
     wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
-    _check(lib().mapl_norm_bwd(ctypes.byref(D), _ptr(dy), _ptr(dxo), _ptr(xo), _ptr(h), _ptr(gate), _ptr(w_post),
-                               _ptr(scale), _ptr(w_pre), _ptr(dx), _ptr(dh), _ptr(dgate), _ptr(dw_post), _ptr(dscale),
-                               _ptr(dw_pre), int(accumulate_dw), _ptr(ws), wb, _stream(stream)))
+    _check(lib().mapl_norm_bwd(ctypes.byref(D), *_ptrs(dy, dxo, xo, h, gate, w_post, scale, w_pre, dx, dh, dgate, dw_post,
+                                                       dscale, dw_pre), int(accumulate_dw), _ptr(ws), wb, _stream(stream)))
 
 
 class OptimParams:
     """A host array of mapl_param and the tensors that it points to (kept alive with it);
-    sizes: the bytes of a value of each kind (None: not given), which the calls look at."""
+    sizes: the bytes of a value of each kind that is given, which the calls look at."""
 
     def __init__(self, array, count, tensors, sizes=None):
         self.array, self.count, self.tensors, self.sizes = array, count, tensors, sizes or {}
+        self.seen = set()
 
-    def need(self, **sizes):
-        for name, size in sizes.items():
-            if self.sizes.get(name, size) not in (None, size):
+    def need(self, *sizes):
+        """Looks once whether the arrays have values of these sizes: (name, bytes) each."""
+        if sizes in self.seen:
+            return
+        for name, size in sizes:
+            if self.sizes.get(name, size) != size:
                 raise ValueError("%s has values of %d bytes, this call takes %d" % (name, self.sizes[name], size))
+        self.seen.add(sizes)
 
 
 def optim_params(g, p=None, m=None, v=None, e=None, p16=None, weight_decay=0.0, lr_scale=1.0):
@@ -434,7 +442,7 @@ def grad_norm_workspace_bytes(params, g_dtype="f32"):
 
 def grad_norm(params, stats, ws, step=None, grad_scale=1.0, max_norm=float("inf"), g_dtype="f32", ws_bytes=None, stream=None):
     """stats[0]: the norm of all gradients, stats[1]: the factor that clips them; counts step up if it is finite."""
-    params.need(g=2 if g_dtype in ("bf16", BF16) else 4)
+    params.need(("g", 2 if g_dtype in ("bf16", BF16) else 4))
     wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
     _check(lib().mapl_grad_norm(params.array, params.count, _DT.get(g_dtype, g_dtype), grad_scale, max_norm, _ptr(stats),
                                 _ptr(step), _ptr(ws), wb, _stream(stream)))
@@ -448,7 +456,7 @@ def adamw_desc(lr, beta1=0.9, beta2=0.95, eps=1e-8, g_dtype="f32", states="f32",
 def adamw_step(A, params, stats=None, step=None, lr=None, stream=None):
     """One step over all of params; stats as grad_norm leaves it, step (int32) and lr (fp32) on the device."""
     state = 1 if A.states == STATES_8BIT else 4
-    params.need(g=2 if A.g_dtype == BF16 else 4, p=4, m=state, v=state, e=1, p16=2)
+    params.need(("g", 2 if A.g_dtype == BF16 else 4), ("p", 4), ("m", state), ("v", state), ("e", 1), ("p16", 2))
     _check(lib().mapl_adamw_step(ctypes.byref(A), params.array, params.count, _ptr(stats), _ptr(step), _ptr(lr),
                                  _stream(stream)))
 
@@ -457,8 +465,8 @@ def adamw_unpack(packed, values, stream=None):
     """The values of 8-bit states, as fp32 m and v."""
     if packed.count != values.count:
         raise ValueError("%d and %d tensors" % (packed.count, values.count))
-    packed.need(m=1, v=1, e=1)
-    values.need(m=4, v=4)
+    packed.need(("m", 1), ("v", 1), ("e", 1))
+    values.need(("m", 4), ("v", 4))
     _check(lib().mapl_adamw_unpack(packed.array, values.array, packed.count, _stream(stream)))
 
 
@@ -466,8 +474,8 @@ def adamw_pack(values, packed, stream=None):
     """fp32 m and v in 8 bits, rounded to nearest."""
     if packed.count != values.count:
         raise ValueError("%d and %d tensors" % (packed.count, values.count))
-    packed.need(m=1, v=1, e=1)
-    values.need(m=4, v=4)
+    packed.need(("m", 1), ("v", 1), ("e", 1))
+    values.need(("m", 4), ("v", 4))
     _check(lib().mapl_adamw_pack(values.array, packed.array, packed.count, _stream(stream)))
 
 

@@ -56,10 +56,12 @@ def norm_y(xo, w_pre, eps):
 R = 36 * U24
 
 
-def norm_fwd_errors(x, xo, t, y, pre_dt):
-    """Bounds of |x' - form| and |y - norm_y(x')|: t has r, three products, act (8 u)
-    and the sum's rounding; y r and two products; each its type's rounding."""
-    e_x = (R + 16 * U24) * t + U24 * (x.double().abs() + t) + 1.01 * half_step(x.dtype) * xo.abs()
+def norm_fwd_errors(x, xo, t, y, pre_dt, G=None):
+    """Bounds of |x' - form| and |y - norm_y(x')|: t has r, three products, act (8 u, and a
+    bf16 gate's exponent is off by 1.3 |G| u) and the sum's rounding; y r and two products; each
+    its type's rounding."""
+    gate = 1.3 * U24 * G.double().abs() if G is not None and G.dtype == torch.bfloat16 else 0.0
+    e_x = (R + 16 * U24 + gate) * t + U24 * (x.double().abs() + t) + 1.01 * half_step(x.dtype) * xo.abs()
     e_y = None if y is None else (R + 4 * U24 + 1.01 * half_step(pre_dt)) * y.abs() + 1e-40
     return e_x + 1e-40, e_y
 
@@ -94,9 +96,10 @@ def norm_bwd(dy, dxo, xo, h, G, w_post, scale, w_pre, kind, post, alpha, eps):
         by = alpha * _vec(scale)
         o["dscale"] = (alpha * dx * n * f).sum(0)
         o["e_dscale"] = chain * (abs(alpha) * A * (n * f).abs()).sum(0)
+        gate = 2.6 * U24 * G.double().abs() if kind != "none" and G.dtype == torch.bfloat16 else 0.0  # (act and 1 - sigmoid)
         if kind != "none":
             o["dgate"] = by * dx * n * df
-            o["e_dgate"] = (4 * R + 120 * U24) * A * (by * n * dfa).abs()
+            o["e_dgate"] = (4 * R + 120 * U24 + gate) * A * (by * n * dfa).abs()
         dn = by * dx * f
         if post:
             o["dw_post"] = (dn * h * r).sum(0)

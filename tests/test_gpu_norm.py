@@ -73,7 +73,7 @@ class Case:
         xo = self.x
         if self.branch:
             ref, t = sh.norm_fwd(self.x, self.h, self.G, self.w_post, self.scale, self.kind, self.post, self.alpha, self.eps)
-            within(self.xo, ref, sh.norm_fwd_errors(self.x, ref, t, None, None)[0], "xo")
+            within(self.xo, ref, sh.norm_fwd_errors(self.x, ref, t, None, None, self.G)[0], "xo")
             xo = self.xo
         if self.pre:
             y = sh.norm_y(xo, self.w_pre, self.eps)

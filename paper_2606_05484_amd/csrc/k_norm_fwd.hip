@@ -20,9 +20,9 @@ namespace {
 
 // A row is held by LANES lanes, eight values NV times each; a workgroup of THREADS
 // takes THREADS / LANES rows.
-template <typename X, typename H, int LANES, int NV, bool BRANCH, bool PRE, int GATE, bool ONCE>
-__global__ __launch_bounds__(norm_threads(LANES)) void k_norm_fwd(const NormArgs g) {
-  constexpr int THREADS = norm_threads(LANES), ROWS = THREADS / LANES;
+template <typename X, typename H, int LANES, int NV, int THREADS, bool BRANCH, bool PRE, int GATE, bool ONCE>
+__global__ __launch_bounds__(THREADS) void k_norm_fwd(const NormArgs g) {
+  constexpr int ROWS = THREADS / LANES;
   constexpr bool SPLIT = sizeof(X) == 4, FINE = sizeof(H) == 4;
   __shared__ float lds[sums_floats(LANES, ROWS)];
   int turn = 0;
@@ -109,19 +109,19 @@ __global__ __launch_bounds__(norm_threads(LANES)) void k_norm_fwd(const NormArgs
   }
 }
 
-template <typename X, typename H, int LANES, int NV, bool ONCE>
+template <typename X, typename H, int LANES, int NV, int THREADS, bool ONCE>
 hipError_t run(const NormArgs& g, hipStream_t s) {
-  constexpr int THREADS = norm_threads(LANES), ROWS = THREADS / LANES;
+  constexpr int ROWS = THREADS / LANES;
   const bool br = g.parts & NORM_BRANCH, pre = g.parts & NORM_PRE;
-  void (*f)(NormArgs) = k_norm_fwd<X, H, LANES, NV, false, true, 0, ONCE>;
+  void (*f)(NormArgs) = k_norm_fwd<X, H, LANES, NV, THREADS, false, true, 0, ONCE>;
   if (br && pre)
-    f = g.act == 0 ? k_norm_fwd<X, H, LANES, NV, true, true, 0, ONCE>
-        : g.act == NORM_SILU ? k_norm_fwd<X, H, LANES, NV, true, true, NORM_SILU, ONCE>
-                             : k_norm_fwd<X, H, LANES, NV, true, true, NORM_SIGMOID, ONCE>;
+    f = g.act == 0 ? k_norm_fwd<X, H, LANES, NV, THREADS, true, true, 0, ONCE>
+        : g.act == NORM_SILU ? k_norm_fwd<X, H, LANES, NV, THREADS, true, true, NORM_SILU, ONCE>
+                             : k_norm_fwd<X, H, LANES, NV, THREADS, true, true, NORM_SIGMOID, ONCE>;
   else if (br)
-    f = g.act == 0 ? k_norm_fwd<X, H, LANES, NV, true, false, 0, ONCE>
-        : g.act == NORM_SILU ? k_norm_fwd<X, H, LANES, NV, true, false, NORM_SILU, ONCE>
-                             : k_norm_fwd<X, H, LANES, NV, true, false, NORM_SIGMOID, ONCE>;
+    f = g.act == 0 ? k_norm_fwd<X, H, LANES, NV, THREADS, true, false, 0, ONCE>
+        : g.act == NORM_SILU ? k_norm_fwd<X, H, LANES, NV, THREADS, true, false, NORM_SILU, ONCE>
+                             : k_norm_fwd<X, H, LANES, NV, THREADS, true, false, NORM_SIGMOID, ONCE>;
   // (a launch holds fewer than 2^32 threads)
   constexpr int64_t MOST = (int64_t)1 << 21;
   for (int64_t t = 0; t < g.T; t += MOST * ROWS) {
@@ -143,14 +143,17 @@ hipError_t run(const NormArgs& g, hipStream_t s) {
 
 template <typename X, typename H, bool ONCE>
 hipError_t pick(const NormArgs& g, hipStream_t s) {
-  if (g.d <= 128) return run<X, H, 16, 1, ONCE>(g, s);
-  if (g.d <= 256) return run<X, H, 32, 1, ONCE>(g, s);
-  if (g.d <= 512) return run<X, H, 64, 1, ONCE>(g, s);
-  if (g.d <= 1024) return run<X, H, 64, 2, ONCE>(g, s);
-  if (g.d <= 2048) return run<X, H, 256, 1, ONCE>(g, s);
-  if (g.d <= 4096) return run<X, H, 256, 2, ONCE>(g, s);
-  if (g.d <= 8192) return run<X, H, 512, 2, ONCE>(g, s);
-  return run<X, H, 1024, 2, ONCE>(g, s);
+  if (g.d <= 64) return run<X, H, 8, 1, 256, ONCE>(g, s);
+  if (g.d <= 128) return run<X, H, 16, 1, 256, ONCE>(g, s);
+  if (g.d <= 256) return run<X, H, 32, 1, 256, ONCE>(g, s);
+  if (g.d <= 512) return run<X, H, 64, 1, 256, ONCE>(g, s);
+  if (g.d <= 1024) return run<X, H, 64, 2, 256, ONCE>(g, s);
+  if (g.d <= 1536) return run<X, H, 192, 1, 192, ONCE>(g, s);
+  if (g.d <= 2048) return run<X, H, 256, 1, 256, ONCE>(g, s);
+  if (g.d <= 2560) return run<X, H, 320, 1, 320, ONCE>(g, s);
+  if (g.d <= 4096) return run<X, H, 256, 2, 256, ONCE>(g, s);
+  if (g.d <= 8192) return run<X, H, 512, 2, 512, ONCE>(g, s);
+  return run<X, H, 1024, 2, 1024, ONCE>(g, s);
 }
 
 }  // namespace

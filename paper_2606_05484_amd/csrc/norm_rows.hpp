@@ -88,6 +88,12 @@ struct Oct<float> {
   __device__ __forceinline__ float get(int i) const { return i < 4 ? a[i] : b[i - 4]; }
   __device__ __forceinline__ void forget() {}
 };
+// Makes f here and now: what it is made of would else be carried past the next branches (sums to
+// the loop's end, stored values to their store), in several times the registers.  For rows that fill them;
+// where there is room the compiler's order is the faster one.
+__device__ __forceinline__ void pin8(float (&f)[8]) {
+  asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]), "+v"(f[4]), "+v"(f[5]), "+v"(f[6]), "+v"(f[7]));
+}
 // (rounds f to what memory holds)
 template <int L, bool S, bool O>
 __device__ __forceinline__ void put8(bf16_t* row, const Cols<L, S, O>& c, int v, float (&f)[8], bool live = true) {
@@ -106,8 +112,9 @@ __device__ __forceinline__ void put8(bf16_t* row, const Cols<L, S, O>& c, int v,
 }
 template <int L, bool S, bool O>
 __device__ __forceinline__ void put8(float* row, const Cols<L, S, O>& c, int v, float (&f)[8], bool live = true) {
-  if (live && c.in(v, 0)) row_store<O>(at_value<f32x4_t>(row, c.at(v, 0)), f32x4_t{f[0], f[1], f[2], f[3]});
-  if (live && c.in(v, 1)) row_store<O>(at_value<f32x4_t>(row, c.at(v, 1)), f32x4_t{f[4], f[5], f[6], f[7]});
+  const f32x4_t a = {f[0], f[1], f[2], f[3]}, b = {f[4], f[5], f[6], f[7]};
+  if (live && c.in(v, 0)) row_store<O>(at_value<f32x4_t>(row, c.at(v, 0)), a);
+  if (live && c.in(v, 1)) row_store<O>(at_value<f32x4_t>(row, c.at(v, 1)), b);
 }
 
 // what a vector that is not given reads as
@@ -120,7 +127,10 @@ static __device__ const struct Ones {
 __device__ __forceinline__ const float* or_ones(const float* w) { return w ? w : ones.v; }
 template <int L, bool S, bool O>
 __device__ __forceinline__ void vec8(const float* w, const Cols<L, S, O>& c, int v, float (&f)[8]) {
-  const f32x4_t a = *at_value<const f32x4_t>(w, c.from(v, 0)), b = *at_value<const f32x4_t>(w, c.from(v, 1));
+  typedef const __attribute__((address_space(1))) char* Global;  // (the ones' or the caller's: global memory either way)
+  typedef const __attribute__((address_space(1))) f32x4_t* Four;
+  const Global p = (Global)(const char*)w;
+  const f32x4_t a = *(Four)(p + 4u * c.from(v, 0)), b = *(Four)(p + 4u * c.from(v, 1));
 #pragma unroll
   for (int i = 0; i < 4; ++i) f[i] = a[i], f[4 + i] = b[i];
 }
@@ -144,7 +154,7 @@ __device__ __forceinline__ uint32_t row_sums(float (&v)[N], float* lds, int& tur
     v[n] = dpp_add<0xB1>(v[n]);   // lane ^ 1
     v[n] = dpp_add<0x4E>(v[n]);   // lane ^ 2
     v[n] = dpp_add<0x141>(v[n]);  // the other half of 8
-    v[n] = dpp_add<0x140>(v[n]);  // the other half of 16
+    if constexpr (LANES >= 16) v[n] = dpp_add<0x140>(v[n]);  // the other half of 16
     if constexpr (LANES == 32) v[n] += __shfl_xor(v[n], 16, WAVE);
     if constexpr (LANES >= 64) v[n] = (lane_of(v[n], 0) + lane_of(v[n], 16)) + (lane_of(v[n], 32) + lane_of(v[n], 48));
     if constexpr (LANES <= 64) over |= v[n] < SUM_LIMIT ? 0u : 1u << n;
@@ -226,8 +236,6 @@ __device__ __forceinline__ void act_both(float g, float& f, float& df) {
   df = KIND == NORM_SILU ? a * fmaf(g, b, 1.f) : a * b;
 }
 
-// threads of a workgroup that gives a row LANES lanes
-constexpr int norm_threads(int lanes) { return lanes > 256 ? lanes : 256; }
 // which of the workgroup's rows (uniform where a wave has one: addresses are then scalar)
 template <int LANES, int ROWS>
 __device__ __forceinline__ int sub_row() {

@@ -237,7 +237,7 @@ struct Four {
       float mj = m[j], vj = v[j];
       state_update(g[j] * a.factor, a.c1, a.c2, mj, vj);
       m[j] = mj, v[j] = vj;
-      s[j] = LOW ? sqrtf(vj) : __builtin_amdgcn_sqrtf(vj);
+      s[j] = sqrtf(vj);  // (v may be subnormal: g past 1e-19 and an eps as small)
       p[j] -= fmaf(a.decay, p[j], a.up * (mj / fmaf(s[j], a.rs, a.eps)));
     }
     put4<ALL, ONCE>(x.p, at, x.n, p);

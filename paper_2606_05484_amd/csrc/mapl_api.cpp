@@ -1936,6 +1936,10 @@ extern "C" int mapl_norm_bwd(const mapl_norm_desc* desc, const void* dy, const v
                    {dw_pre, vb, "dw_pre"}},
                   {{dy, yb, "dy"}, {dxo, xb, "dxo"}, {xo, xb, "xo"}, {h, hb, "h"}, {gate, gb, "gate"},
                    {w_post, vb, "w_post"}, {scale, vb, "scale"}, {w_pre, vb, "w_pre"}, {ws, ws_bytes, "workspace"}});
+  if (!st)
+    st = check_ptrs({}, {{ws, ws_bytes, "workspace"}},
+                    {{dy, yb, "dy"}, {dxo, xb, "dxo"}, {xo, xb, "xo"}, {h, hb, "h"}, {gate, gb, "gate"}, {w_post, vb, "w_post"},
+                     {scale, vb, "scale"}, {w_pre, vb, "w_pre"}});
   if (!st) st = check_ptrs({}, {{dx, xb, "dx"}}, {{dh, hb, "dh"}, {dgate, gb, "dgate"}});
   if (!st)
     st = check_ptrs({}, {{dw_post, vb, "dw_post"}, {dscale, vb, "dscale"}, {dw_pre, vb, "dw_pre"}},

@@ -209,6 +209,20 @@ def test_gradients_of_any_size(size):
             s.check(want)
 
 
+@pytest.mark.parametrize("size,eps", [(1e-20, 1e-24), (1e-21, 1e-21), (1e-10, 1e-24)])
+def test_a_tiny_eps_beside_the_root_of_a_subnormal_number(size, eps):
+    for low in (False, True):
+        s = Stage([3000], low=low, eps=eps)
+        for x in s.m + s.v + (s.e or []):
+            x.zero_()
+        s.G[0].copy_(size * torch.randn(3000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(8)))
+        for t in (1, 2, 3):
+            want = s.expected(t, 1)
+            mapl.adamw_step(s.desc(t, 1), s.params)
+            torch.cuda.synchronize()
+            s.check(want)
+
+
 def test_states_over_many_powers_of_two_in_a_block():
     s = Stage([128 * 40], low=True)
     s.G[0].copy_(torch.randn(128 * 40, device="cuda") * 2.0 ** torch.linspace(-60, 0, 128, device="cuda").repeat(40))

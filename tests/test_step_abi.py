@@ -69,6 +69,12 @@ def test_norm_backward_refusals(kw, status):
     assert mapl.last_error() != ""
 
 
+@pytest.mark.parametrize("given", range(8))
+def test_norm_backward_refuses_a_workspace_over_what_it_reads(given):
+    assert bwd(mapl.norm_desc(64, 128, **WHOLE), ws=P[given] + 256) == -6
+    assert "workspace" in mapl.last_error()
+
+
 @pytest.mark.parametrize("parts,extra", [
     (dict(pre=True), ("h",)), (dict(pre=True), ("scale",)), (dict(pre=True), ("w_post",)), (dict(pre=True), ("xo",)),
     (dict(pre=True), ("gate",)), (dict(pre=False, branch=True), ("y",)), (dict(pre=False, branch=True), ("w_pre",)),

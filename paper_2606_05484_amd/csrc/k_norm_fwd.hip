@@ -11,7 +11,8 @@
 // here 4.9); T = 8192, d = 1024 14.1 us, 5.9 TB/s.  What carried it: one row a wave or a workgroup with all of
 // its loads first and no branch before them (143 us with one around each), rows by a scalar
 // base and 32-bit offsets, one-shot workgroups (with 2048 of them in a loop 150 and 129),
-// fp32 rows in runs of 1 KiB a wave and access.
+// fp32 rows in runs of 1 KiB a wave and access, rows past 8192 on 512 lanes (T = 4096, d = 8256 with
+// 1024 lanes 92 us, 71; d = 12288 113, 90; d = 16384 128, 121).
 #include "norm_rows.hpp"
 
 namespace mapl {
@@ -141,6 +142,8 @@ hipError_t run(const NormArgs& g, hipStream_t s) {
   return hipSuccess;
 }
 
+// The lanes of a row: few enough idle ones, and few enough variants (T = 4096, d = 4160 with 512 lanes 42 us,
+// with 320 37; d = 6144 the same with 384 as with 512).
 template <typename X, typename H, bool ONCE>
 hipError_t pick(const NormArgs& g, hipStream_t s) {
   if (g.d <= 64) return run<X, H, 8, 1, 256, ONCE>(g, s);
@@ -152,8 +155,10 @@ hipError_t pick(const NormArgs& g, hipStream_t s) {
   if (g.d <= 2048) return run<X, H, 256, 1, 256, ONCE>(g, s);
   if (g.d <= 2560) return run<X, H, 320, 1, 320, ONCE>(g, s);
   if (g.d <= 4096) return run<X, H, 256, 2, 256, ONCE>(g, s);
+  if (g.d <= 5120) return run<X, H, 320, 2, 320, ONCE>(g, s);
   if (g.d <= 8192) return run<X, H, 512, 2, 512, ONCE>(g, s);
-  return run<X, H, 1024, 2, 1024, ONCE>(g, s);
+  if (g.d <= 12288) return run<X, H, 512, 3, 512, ONCE>(g, s);
+  return run<X, H, 512, 4, 512, ONCE>(g, s);
 }
 
 }  // namespace

@@ -39,7 +39,8 @@ __global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormArgs g) {
   const float *w_post = or_ones(g.w_post), *scale = or_ones(g.scale), *w_pre = or_ones(g.w_pre);
   // Rows past 8192 values do not stay in registers: what a step needs is loaded again (from the
   // caches) a run of eight at a time.  d = 16384, T = 1024 in bf16: 106 us and 7 for the sum (held, with
-  // spills, 165 to 234).
+  // spills, 165 to 234).  Up to 12288 on 768 lanes, T = 4096, d = 8256 160 us, d = 12288 210 (on 512 lanes
+  // 172 and 212, 253 and 301 with room for 16384; past 12288 1024 lanes spill).
   constexpr bool AGAIN = LANES * NV * 8 > 8192;
   float acc[NS][NV][8];
 #pragma unroll
@@ -265,6 +266,9 @@ hipError_t run(const NormArgs& g, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The lanes of a row: few enough idle ones, and few enough variants.  With the next power of two in
+// their place, T = 8000, us: d = 2112, y alone 38 (320 lanes: 28), d = 1536 gated 54 (192: 50); T = 4096: d = 4160 gated
+// 92 (320 twice: 87), d = 6144 the same with 384 as with 512.
 template <typename X, typename H, bool ONCE>
 hipError_t pick(const NormArgs& g, hipStream_t s) {
   if constexpr (!ONCE) {
@@ -279,7 +283,9 @@ hipError_t pick(const NormArgs& g, hipStream_t s) {
   if (g.d <= 2048) return run<X, H, 256, 1, 256, ONCE>(g, s);
   if (g.d <= 2560) return run<X, H, 320, 1, 320, ONCE>(g, s);
   if (g.d <= 4096) return run<X, H, 256, 2, 256, ONCE>(g, s);
+  if (g.d <= 5120) return run<X, H, 320, 2, 320, ONCE>(g, s);
   if (g.d <= 8192) return run<X, H, 512, 2, 512, ONCE>(g, s);
+  if (g.d <= 12288) return run<X, H, 768, 2, 768, ONCE>(g, s);
   return run<X, H, 512, 4, 512, ONCE>(g, s);
 }
 

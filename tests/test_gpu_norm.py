@@ -95,7 +95,7 @@ def within(got, want, tol, name):
 
 
 SIZES = [(1, 64), (1000, 64), (3, 128), (5, 192), (17, 256), (37, 320), (9, 512), (33, 576), (70, 1024), (1021, 1024), (11, 1088), (300, 1536), (9, 1600), (4, 2048),
-         (1, 2048), (530, 2048), (7, 2112), (600, 2560), (3, 2624), (5, 4096), (3, 4160), (3, 8192), (2, 8256), (300, 8704), (3, 16384), (1, 16384)]
+         (1, 2048), (530, 2048), (7, 2112), (600, 2560), (3, 2624), (5, 4096), (3, 4160), (300, 5120), (2, 5184), (3, 8192), (2, 8256), (300, 8704), (2, 12288), (300, 12352), (3, 16384), (1, 16384)]
 
 
 @pytest.mark.parametrize("T,d", SIZES)

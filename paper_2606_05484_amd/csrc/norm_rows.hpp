@@ -1,5 +1,5 @@
 // What the forward and the backward of the norms around a block (k_norm_fwd.hip,
-// k_norm_bwd.hip) share: how a row of d values lies over lanes, its sums, and the gate.
+// norm_bwd.hpp) share: how a row of d values lies over lanes, its sums, and the gate.
 #pragma once
 #include "common.hpp"
 #include "kernels.hpp"

@@ -354,3 +354,47 @@ def test_past_two_gib():
     o = sh.norm_bwd(y[rows], None, few, None, None, None, None, w, "none", False, 1.0, 1e-5)
     within(dx[rows], o["dx"], o["e_dx"] + 1.01 * sh.UB * o["dx"].abs() + 1e-38, "dx")
     within(dw, o["dw_pre"], o["e_dw_pre"] * (1 + T / 256 / 500) + 1e-38, "dw_pre")
+
+
+@pytest.mark.parametrize("d", [64, 128, 256, 512, 1024, 1536, 2048, 2560, 4096, 5120, 8192, 12288, 16384])
+@pytest.mark.parametrize("T", [1, 5, 1030])
+def test_rows_behind_the_last_one_and_bytes_behind_the_workspace(T, d):
+    """Arrays of more rows than the call has: those hold NaNs, are not read and not written; a
+    workspace of just the bytes that are asked for."""
+    if T * d > 1 << 22:
+        T = 70
+    c, more = Case(T, d, gate="silu"), 9
+    names = ("x", "h", "G", "dy", "dxo", "xo", "y", "dx", "dh", "dG")
+    whole = {}
+    for name in names:
+        part = getattr(c, name)
+        whole[name] = torch.full((T + more, d), float("nan"), dtype=part.dtype, device="cuda")
+        whole[name][:T] = part
+        setattr(c, name, whole[name][:T])
+    need = mapl.norm_workspace_bytes(c.D)
+    c.ws = torch.full((need + 65536,), 90, dtype=torch.uint8, device="cuda")
+    c.fwd()
+    c.bwd(ws_bytes=need)
+    torch.cuda.synchronize()
+    assert all(t[T:].isnan().all() for t in whole.values()) and (c.ws[need:] == 90).all()
+    c.check()
+
+
+def test_two_calls_at_once():
+    """Two streams side by side, each with its own arrays and workspace."""
+    cases = [Case(3000, 1024, gate="silu", seed=1), Case(2000, 2048, "f32", "bf16", seed=2)]
+    want = []
+    for c in cases:
+        c.fwd()
+        c.bwd()
+        torch.cuda.synchronize()
+        want.append(c.outputs())
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(10):
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                c.fwd()
+                c.bwd()
+    torch.cuda.synchronize()
+    for c, w in zip(cases, want):
+        assert all(torch.equal(v, w[k]) for k, v in c.outputs().items())

@@ -408,3 +408,36 @@ def test_past_two_to_the_32():
     assert abs(float(stats[0]) - math.sqrt(91.0)) < 1e-6
     assert torch.allclose(P[at], torch.tensor([-0.5, 0.5, -0.5, 0.5, -0.5, 0.5], device="cuda"), rtol=1e-6)
     assert int((P != 0).sum()) == len(at)
+
+
+@pytest.mark.parametrize("sizes", [[1], [4096 * 3000 + 1], [5000] * 60])
+def test_bytes_behind_the_norms_workspace(sizes):
+    G = grads(sizes, "f32", 3)
+    p = mapl.optim_params(G)
+    need = mapl.grad_norm_workspace_bytes(p)
+    ws = torch.full((need + 65536,), 90, dtype=torch.uint8, device="cuda")
+    stats = torch.full((8,), 7.0, device="cuda")
+    mapl.grad_norm(p, stats, ws, ws_bytes=need)
+    torch.cuda.synchronize()
+    assert (ws[need:] == 90).all() and (stats[2:] == 7.0).all()
+    norm = math.sqrt(sum(float(g.double().square().sum()) for g in G))
+    assert abs(float(stats[0]) - norm) <= 2.0 ** -23 * norm and float(stats[1]) == 1.0
+
+
+@pytest.mark.parametrize("low", [False, True], ids=["f32", "8bit"])
+def test_two_steps_at_once(low):
+    """Two streams side by side, each with its own tensors."""
+    a, b = [Stage(SIZES, low=low, seed=k) for k in (1, 2)], [Stage(SIZES, low=low, seed=k) for k in (1, 2)]
+    torch.cuda.synchronize()
+    for t in range(1, 6):
+        for s in a:
+            mapl.adamw_step(s.desc(t, 4), s.params)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in b]
+    for t in range(1, 6):
+        for s, on in zip(b, streams):
+            with torch.cuda.stream(on):
+                mapl.adamw_step(s.desc(t, 4), s.params)
+    torch.cuda.synchronize()
+    for x, y in zip(a, b):
+        assert all(torch.equal(p, q) for p, q in zip(x.everything(), y.everything()))

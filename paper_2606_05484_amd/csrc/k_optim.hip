@@ -2,7 +2,7 @@
 // with the factor that clips it, and AdamW with states in fp32 or in 8 bits:
 //   g' = factor g,  m <- m + (1 - b1)(g' - m),  v <- v + (1 - b2)(g'^2 - v)
 //   p <- p - (lr wd p + lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps))
-// A launch takes up to OPTIM_TENSORS tensors from its arguments and cuts them in
+// A launch takes up to 52 tensors (the norm 176) from its arguments and cuts them in
 // pieces of OPTIM_PIECE values, one a workgroup, so that many small tensors and a
 // large one fill the chip alike.
 //
@@ -41,13 +41,18 @@ __device__ __forceinline__ uint32_t hash32(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-// the tensor that a piece belongs to (uniform): every lane looks at one (a search would
+// the tensor that a piece belongs to (uniform): every lane looks at one or a few (a search would
 // wait for its loads in turn)
-__device__ __forceinline__ int tensor_of(const OptimTable& t, uint32_t piece) {
-  static_assert(OPTIM_TENSORS < WAVE, "a lane for each");
+template <typename Table>
+__device__ __forceinline__ int tensor_of(const Table& t, uint32_t piece) {
   const int l = threadIdx.x & 63;
-  const bool below = l < t.count && t.first[l] <= piece;
-  return __builtin_amdgcn_readfirstlane(__builtin_popcountll(__ballot(below)) - 1);
+  int i = -1;
+#pragma unroll
+  for (int k = 0; k < Table::MOST; k += WAVE) {
+    const bool below = k + l < t.count && t.first[k + l] <= piece;
+    i += __builtin_popcountll(__ballot(below));
+  }
+  return __builtin_amdgcn_readfirstlane(i);
 }
 
 // Values i .. i + 3 of n, a lane's share: a wave's 16-byte accesses are whole runs of
@@ -373,7 +378,7 @@ __device__ __forceinline__ double wave_sum64(double v) {
 // order, which the launch fixes, shows in no digit of the norm.  266 M bf16 values 79 us, 6.7 TB/s
 // (with 1024 workgroups 103).
 template <typename G, bool ONCE>
-__global__ __launch_bounds__(256) void k_grad_squares(const OptimTable t, double* __restrict__ part) {
+__global__ __launch_bounds__(256) void k_grad_squares(const GradTable t, double* __restrict__ part) {
   __shared__ double w[4];
   double s = 0.0;
   for (uint32_t piece = blockIdx.x; piece < t.first[t.count]; piece += gridDim.x) {
@@ -426,8 +431,8 @@ __global__ __launch_bounds__(512) void k_grad_norm(const double* __restrict__ pa
 int64_t optim_pieces(int64_t n) { return (n + OPTIM_PIECE - 1) / OPTIM_PIECE; }
 int grad_norm_parts(int64_t pieces) { return (int)(pieces < GRAD_WGS ? pieces : GRAD_WGS); }
 
-hipError_t launch_grad_squares(const OptimTable& t, int g_f32, int once, double* part, hipStream_t s) {
-  void (*f)(OptimTable, double*) = g_f32 ? once ? k_grad_squares<float, true> : k_grad_squares<float, false>
+hipError_t launch_grad_squares(const GradTable& t, int g_f32, int once, double* part, hipStream_t s) {
+  void (*f)(GradTable, double*) = g_f32 ? once ? k_grad_squares<float, true> : k_grad_squares<float, false>
                                          : once ? k_grad_squares<bf16_t, true> : k_grad_squares<bf16_t, false>;
   hipLaunchKernelGGL(f, dim3(grad_norm_parts(t.first[t.count])), dim3(256), 0, s, t, part);
   return hipGetLastError();

@@ -441,25 +441,32 @@ struct NormSums {
 hipError_t launch_norm_sum(const float* part, int n, int d, const NormSums& o, int add, hipStream_t s);
 
 // ---------------------------------------------------------------- optimizer
-// One tensor of a step; a launch takes up to OPTIM_TENSORS of them in its
+// One tensor of a step; a launch takes a table of them in its
 // arguments (no table in memory that would have to be copied or outlive the call).
 struct OptimTensor {
   float* p; const void* g; void* m; void* v; uint8_t* e; bf16_t* p16;
   int64_t n;
   float weight_decay, lr_scale;
 };
-constexpr int OPTIM_TENSORS = 52;
-struct OptimTable {
-  OptimTensor t[OPTIM_TENSORS];
-  uint32_t first[OPTIM_TENSORS + 1];  // the workgroups' pieces: tensor i has first[i] .. first[i + 1] - 1
+template <typename Tensor, int N>
+struct PieceTable {
+  static constexpr int MOST = N;
+  Tensor t[N];
+  uint32_t first[N + 1];  // the workgroups' pieces: tensor i has first[i] .. first[i + 1] - 1
   int count;
   uint32_t index;  // the first tensor's in the whole call
 };
+struct GradTensor {
+  const void* g;
+  int64_t n;
+};
+typedef PieceTable<OptimTensor, 52> OptimTable;
+typedef PieceTable<GradTensor, 176> GradTable;  // (what the gradients' norm reads, in as many bytes)
 int64_t optim_pieces(int64_t n);
 // part[0 .. grad_norm_parts(pieces) - 1]: sums of squares (64 bits)
 int grad_norm_parts(int64_t pieces);
 // once: nothing finds these lines in a cache again before others have taken their place
-hipError_t launch_grad_squares(const OptimTable& t, int g_f32, int once, double* part, hipStream_t s);
+hipError_t launch_grad_squares(const GradTable& t, int g_f32, int once, double* part, hipStream_t s);
 hipError_t launch_grad_norm(const double* part, int n, float grad_scale, float max_norm, float* stats, int32_t* step,
                             hipStream_t s);
 struct AdamwArgs {

@@ -2079,20 +2079,19 @@ int check_g_dtype(int g_dtype) {
   return MAPL_OK;
 }
 
-// Calls f(table) for the tensors in turn, as many as a launch takes at a time.
-template <typename F>
-int for_tables(const mapl_param* params, const mapl_param* values, int64_t count, F&& f) {
-  OptimTable t;
+// Calls f(table) for the tensors in turn, as many as a launch takes at a time; tensor(i): its entry.
+template <typename Table, typename Tensor, typename F>
+int for_tables(const mapl_param* params, int64_t count, Tensor&& tensor, F&& f) {
+  Table t;
   for (int64_t i = 0; i < count;) {
     t.count = 0;
     t.index = (uint32_t)i;
     t.first[0] = 0;
-    for (; t.count < OPTIM_TENSORS && i < count; ++i) {
-      const mapl_param& p = params[i];
-      if (t.count && t.first[t.count] + optim_pieces(p.n) > ((int64_t)1 << 22)) break;  // (fewer than 2^32 threads a launch)
-      t.t[t.count] = {p.p, p.g, p.m, p.v, p.e, (bf16_t*)p.p16, p.n, p.weight_decay, p.lr_scale};
-      if (values) t.t[t.count].p = (float*)values[i].m, t.t[t.count].g = values[i].v;
-      t.first[t.count + 1] = t.first[t.count] + (uint32_t)optim_pieces(p.n);
+    for (; t.count < Table::MOST && i < count; ++i) {
+      const int64_t pieces = optim_pieces(params[i].n);
+      if (t.count && t.first[t.count] + pieces > ((int64_t)1 << 22)) break;  // (fewer than 2^32 threads a launch)
+      t.t[t.count] = tensor(i);
+      t.first[t.count + 1] = t.first[t.count] + (uint32_t)pieces;
       ++t.count;
     }
     if (t.first[t.count] == 0) continue;
@@ -2100,6 +2099,13 @@ int for_tables(const mapl_param* params, const mapl_param* values, int64_t count
     if (st) return st;
   }
   return MAPL_OK;
+}
+template <typename F>
+int for_gradients(const mapl_param* params, int64_t count, F&& f) {
+  return for_tables<GradTable>(params, count, [&](int64_t i) { return GradTensor{params[i].g, params[i].n}; }, f);
+}
+OptimTensor optim_tensor(const mapl_param& p) {
+  return {p.p, p.g, p.m, p.v, p.e, (bf16_t*)p.p16, p.n, p.weight_decay, p.lr_scale};
 }
 
 // Whether a call's arrays, `bytes` a value, are more than the last-level cache (256 MiB) will keep
@@ -2115,7 +2121,7 @@ int streams(const mapl_param* params, int64_t count, int64_t bytes) {
 
 int64_t grad_parts(const mapl_param* params, int64_t count) {
   int64_t n = 0;
-  for_tables(params, nullptr, count, [&](const OptimTable& t) {
+  for_gradients(params, count, [&](const GradTable& t) {
     n += grad_norm_parts(t.first[t.count]);
     return (int)MAPL_OK;
   });
@@ -2145,7 +2151,12 @@ int convert_states(const mapl_param* packed, const mapl_param* values, int64_t c
   });
   if (st) return st;
   hipStream_t s = (hipStream_t)stream;
-  return for_tables(packed, values, count, [&](const OptimTable& t) {
+  const auto tensor = [&](int64_t i) {
+    OptimTensor t = optim_tensor(packed[i]);
+    t.p = (float*)values[i].m, t.g = values[i].v;
+    return t;
+  };
+  return for_tables<OptimTable>(packed, count, tensor, [&](const OptimTable& t) {
     if (pack)
       LAUNCH("adamw:pack", launch_adamw_pack(t, s));
     else
@@ -2186,7 +2197,7 @@ extern "C" int mapl_grad_norm(const mapl_param* params, int64_t count, int32_t g
   double* part = (double*)ws;
   int64_t n = 0;
   const int once = streams(params, count, (int64_t)esize(g_dtype));
-  st = for_tables(params, nullptr, count, [&](const OptimTable& t) {
+  st = for_gradients(params, count, [&](const GradTable& t) {
     LAUNCH("grad_norm:squares", launch_grad_squares(t, g_dtype == MAPL_F32, once, part + n, s));
     n += grad_norm_parts(t.first[t.count]);
     return (int)MAPL_OK;
@@ -2240,7 +2251,7 @@ extern "C" int mapl_adamw_step(const mapl_adamw_desc* desc, const mapl_param* pa
   a.g_f32 = D.g_dtype == MAPL_F32; a.low = low; a.once = streams(params, count, (low ? 12 : 24) + (int64_t)esize(D.g_dtype)); a.step = D.step; a.seed = D.seed;
   a.stats = stats; a.step_at = step; a.lr_at = lr;
   hipStream_t s = (hipStream_t)stream;
-  return for_tables(params, nullptr, count, [&](const OptimTable& t) {
+  return for_tables<OptimTable>(params, count, [&](int64_t i) { return optim_tensor(params[i]); }, [&](const OptimTable& t) {
     LAUNCH("adamw:step", launch_adamw(t, a, s));
     return (int)MAPL_OK;
   });

@@ -24,7 +24,7 @@ def grads(sizes, dt, seed=0, size=1e-3):
 
 # ------------------------------------------------------------------- norm
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
-@pytest.mark.parametrize("sizes", [[1], SIZES, [0, 5, 0], [33] * 160, [], [3000001, 17]], ids=lambda s: "%d_tensors_%d" % (len(s), sum(s)))
+@pytest.mark.parametrize("sizes", [[1], SIZES, [0, 5, 0], [33] * 160, [], [3000001, 17], [0, 4097, 33] * 150], ids=lambda s: "%d_tensors_%d" % (len(s), sum(s)))
 def test_norm(dt, sizes):
     print("grad norm", dt, sizes[:20], flush=True)
     G = grads(sizes, dt)
@@ -410,7 +410,7 @@ def test_past_two_to_the_32():
     assert int((P != 0).sum()) == len(at)
 
 
-@pytest.mark.parametrize("sizes", [[1], [4096 * 3000 + 1], [5000] * 60])
+@pytest.mark.parametrize("sizes", [[1], [4096 * 3000 + 1], [5000] * 60, [5000] * 360])
 def test_bytes_behind_the_norms_workspace(sizes):
     G = grads(sizes, "f32", 3)
     p = mapl.optim_params(G)

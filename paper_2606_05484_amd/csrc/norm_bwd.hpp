@@ -141,7 +141,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormArgs g) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float z = x[v].get(i), y = dy[v].get(i);
-          acc[2 - S0][v][i] = fmaf(y * r, z, acc[2 - S0][v][i]);
+          acc[2 - S0][v][i] = fmaf(z * r, y, acc[2 - S0][v][i]);  // (y r may underflow where z is large)
           q[v][i] = fmaf(r, fmaf(-z, k, y * wp[i]), dxo[v].get(i));
           o[i] = q[v][i];
         }

@@ -24,7 +24,7 @@ namespace {
 template <typename X, typename H, int LANES, int NV, int THREADS, bool BRANCH, bool PRE, int GATE, bool ONCE>
 __global__ __launch_bounds__(THREADS) void k_norm_fwd(const NormArgs g) {
   constexpr int ROWS = THREADS / LANES;
-  constexpr bool SPLIT = sizeof(X) == 4, FINE = sizeof(H) == 4;
+  constexpr bool SPLIT = sizeof(X) == 4, FINE = sizeof(X) == 4;
   __shared__ float lds[sums_floats(LANES, ROWS)];
   int turn = 0;
   const Cols<LANES, SPLIT, ONCE> c{(int)threadIdx.x % LANES, g.d};

@@ -26,7 +26,7 @@ namespace {
 template <typename X, typename H, int LANES, int NV, int THREADS, bool BRANCH, bool PRE, int GATE, bool ONCE>
 __global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormArgs g) {
   constexpr int ROWS = THREADS / LANES;
-  constexpr bool SPLIT = sizeof(X) == 4, FINE = sizeof(H) == 4;
+  constexpr bool SPLIT = sizeof(X) == 4, FINE = sizeof(X) == 4;
   constexpr int NS = (BRANCH ? 2 : 0) + (PRE ? 1 : 0), S0 = BRANCH ? 0 : 2;  // sums: dw_post, ds, dw_pre
   __shared__ float lds[sums_floats(LANES, ROWS)];
   __shared__ float red[ROWS > 1 ? NS * LANES * NV * 8 : 1];

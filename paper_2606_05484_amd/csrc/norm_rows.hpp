@@ -210,9 +210,12 @@ __device__ __forceinline__ float row_scale(float ss, uint32_t over, Z z, float i
 }
 
 // sigmoid(g) = 1 / (1 + e) and 1 - sigmoid(g) = e / (1 + e) with e = exp(-g), each to a few of
-// its last digits at either end (and 1 where e overflows).  FINE (fp32 gates): the
+// its last digits at either end (and 1 where e overflows).  FINE (an fp32 stream): the
 // rounding of -g log2(e), which is |g| units of e's last digit, put right to first order,
-// and the reciprocal with a Newton step.
+// and the reciprocal with a Newton step.  A bf16 stream goes without: its values' own rounding is 2^16
+// of those units, and the vectors' gradients are off by up to 1.3 |g| of them a term.  It would cost,
+// T = 32768, d = 2048 gated, 230 us in place of 201 backward and 119 in place of 117 forward; an fp32 stream
+// with a bf16 block, T = 16384: backward 136 with it and 142 without, forward 83 and 82.
 template <bool FINE>
 __device__ __forceinline__ void sigmoid2(float g, float& a, float& b) {
   constexpr float L = -1.44269504088896341f;

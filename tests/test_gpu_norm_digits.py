@@ -3,7 +3,8 @@ bound (_step_helpers), nothing lost to a product that falls below fp32 on the wa
 import pytest
 import torch
 
-from test_gpu_norm import Case
+import _step_helpers as sh
+from test_gpu_norm import Case, within
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +27,31 @@ def test_small_gradients_of_large_rows(T, d, x, h, size, small, kw):
     torch.cuda.synchronize()
     assert float(c.dw_pre.abs().max()) > 0.1 * small
     c.check()
+
+
+# act(G) alone: x = 0, h = 1 and no norm leave x' = alpha s act(G) in fp32, off by act's error (8 u: the exponential's two, its
+# correction, 1 + e, the reciprocal and their steps, the products), two products and the sum's rounding.
+@pytest.mark.parametrize("h", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["sigmoid", "silu"])
+def test_an_fp32_stream_has_the_gates_digits(h, kind):
+    T, d = 5, 1024
+    c = Case(T, d, "f32", h, post=False, gate=kind)
+    c.x.zero_(), c.h.fill_(1.0)
+    c.G.copy_(torch.linspace(-85, 85, T * d, device="cuda").view(T, d))
+    c.fwd()
+    torch.cuda.synchronize()
+    want = c.alpha * c.scale.double() * sh.act(c.G, kind)[0]
+    within(c.xo, want, 11.01 * sh.U24 * want.abs() + 1e-38, "xo")
+
+
+@pytest.mark.parametrize("h", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["sigmoid", "silu"])
+def test_an_fp32_streams_scale_gradient_has_the_gates_digits(h, kind):
+    """One token: dscale = alpha dx' h act(G), no sum to hide in."""
+    d = 4096
+    c = Case(1, d, "f32", h, post=False, pre=False, gate=kind)
+    c.G.copy_(torch.linspace(-85, 85, d, device="cuda").view(1, d))
+    c.bwd()
+    torch.cuda.synchronize()
+    want = (c.alpha * c.dxo.double() * c.h.double() * sh.act(c.G, kind)[0])[0]
+    within(c.dscale, want, 11.01 * sh.U24 * want.abs() + 1e-38, "dscale")

@@ -373,22 +373,30 @@ def norm_bwd(D, dy, dxo, xo, h, gate, w_post, scale, w_pre, dx, dh, dgate, dw_po
                                                        dscale, dw_pre), int(accumulate_dw), _ptr(ws), wb, _stream(stream)))
 
 
+def _type_name(t):
+    """The name that _DT gives a tensor's type ("u8" for any of one byte), or torch's."""
+    if t.element_size() == 1:
+        return "u8"
+    name = str(t.dtype)
+    return {"torch.float32": "f32", "torch.bfloat16": "bf16"}.get(name, name)
+
+
 class OptimParams:
     """A host array of mapl_param and the tensors that it points to (kept alive with it);
-    sizes: the bytes of a value of each kind that is given, which the calls look at."""
+    types: the type of each kind that is given (_type_name), which the calls look at."""
 
-    def __init__(self, array, count, tensors, sizes=None):
-        self.array, self.count, self.tensors, self.sizes = array, count, tensors, sizes or {}
+    def __init__(self, array, count, tensors, types=None):
+        self.array, self.count, self.tensors, self.types = array, count, tensors, types or {}
         self.seen = set()
 
-    def need(self, *sizes):
-        """Looks once whether the arrays have values of these sizes: (name, bytes) each."""
-        if sizes in self.seen:
+    def need(self, *types):
+        """Looks once whether the arrays have values of these types: (name, type) each."""
+        if types in self.seen:
             return
-        for name, size in sizes:
-            if self.sizes.get(name, size) != size:
-                raise ValueError("%s has values of %d bytes, this call takes %d" % (name, self.sizes[name], size))
-        self.seen.add(sizes)
+        for name, want in types:
+            if self.types.get(name, want) != want:
+                raise ValueError("%s has values of type %s, this call takes %s" % (name, self.types[name], want))
+        self.seen.add(types)
 
 
 def optim_params(g, p=None, m=None, v=None, e=None, p16=None, weight_decay=0.0, lr_scale=1.0):
@@ -402,17 +410,19 @@ def optim_params(g, p=None, m=None, v=None, e=None, p16=None, weight_decay=0.0, 
         if x is not None and len(x) != count:
             raise ValueError("%s has %d entries, g %d" % (name, len(x), count))
     sizes = [t.numel() for t in g]
-    where, bytes_of = {}, {}
+    where, types = {}, {}
     for name, x in lists.items():
         if x is None:
             where[name] = [0] * count
             continue
+        last = None
         for i, t in enumerate(x):
             if t is None:
                 continue
-            size = t.element_size()
-            if bytes_of.setdefault(name, size) != size:
-                raise ValueError("%s has values of %d and of %d bytes" % (name, bytes_of[name], size))
+            if t.dtype is not last:
+                last, kind = t.dtype, _type_name(t)
+                if types.setdefault(name, kind) != kind:
+                    raise ValueError("%s has values of type %s and %s" % (name, types[name], kind))
             if not t.is_contiguous():
                 raise ValueError("%s[%d] is not contiguous" % (name, i))
             if name == "e":
@@ -425,7 +435,7 @@ def optim_params(g, p=None, m=None, v=None, e=None, p16=None, weight_decay=0.0, 
     one = struct.Struct("=q6Q2f")  # Param's layout
     for i, row in enumerate(zip(sizes, *(where[name] for name, _ in Param._fields_[1:7]), decay, lr)):
         one.pack_into(a, i * one.size, *row)
-    return OptimParams(a, count, lists, bytes_of)
+    return OptimParams(a, count, lists, types)
 
 
 def optim_exponents(n):
@@ -442,7 +452,7 @@ def grad_norm_workspace_bytes(params, g_dtype="f32"):
 
 def grad_norm(params, stats, ws, step=None, grad_scale=1.0, max_norm=float("inf"), g_dtype="f32", ws_bytes=None, stream=None):
     """stats[0]: the norm of all gradients, stats[1]: the factor that clips them; counts step up if it is finite."""
-    params.need(("g", 2 if g_dtype in ("bf16", BF16) else 4))
+    params.need(("g", "bf16" if g_dtype in ("bf16", BF16) else "f32"))
     wb = ws_bytes if ws_bytes is not None else (ws.numel() if ws is not None else 0)
     _check(lib().mapl_grad_norm(params.array, params.count, _DT.get(g_dtype, g_dtype), grad_scale, max_norm, _ptr(stats),
                                 _ptr(step), _ptr(ws), wb, _stream(stream)))
@@ -455,8 +465,8 @@ def adamw_desc(lr, beta1=0.9, beta2=0.95, eps=1e-8, g_dtype="f32", states="f32",
 
 def adamw_step(A, params, stats=None, step=None, lr=None, stream=None):
     """One step over all of params; stats as grad_norm leaves it, step (int32) and lr (fp32) on the device."""
-    state = 1 if A.states == STATES_8BIT else 4
-    params.need(("g", 2 if A.g_dtype == BF16 else 4), ("p", 4), ("m", state), ("v", state), ("e", 1), ("p16", 2))
+    state = "u8" if A.states == STATES_8BIT else "f32"
+    params.need(("g", "bf16" if A.g_dtype == BF16 else "f32"), ("p", "f32"), ("m", state), ("v", state), ("e", "u8"), ("p16", "bf16"))
     _check(lib().mapl_adamw_step(ctypes.byref(A), params.array, params.count, _ptr(stats), _ptr(step), _ptr(lr),
                                  _stream(stream)))
 
@@ -465,8 +475,8 @@ def adamw_unpack(packed, values, stream=None):
     """The values of 8-bit states, as fp32 m and v."""
     if packed.count != values.count:
         raise ValueError("%d and %d tensors" % (packed.count, values.count))
-    packed.need(("m", 1), ("v", 1), ("e", 1))
-    values.need(("m", 4), ("v", 4))
+    packed.need(("m", "u8"), ("v", "u8"), ("e", "u8"))
+    values.need(("m", "f32"), ("v", "f32"))
     _check(lib().mapl_adamw_unpack(packed.array, values.array, packed.count, _stream(stream)))
 
 
@@ -474,8 +484,8 @@ def adamw_pack(values, packed, stream=None):
     """fp32 m and v in 8 bits, rounded to nearest."""
     if packed.count != values.count:
         raise ValueError("%d and %d tensors" % (packed.count, values.count))
-    packed.need(("m", 1), ("v", 1), ("e", 1))
-    values.need(("m", 4), ("v", 4))
+    packed.need(("m", "u8"), ("v", "u8"), ("e", "u8"))
+    values.need(("m", "f32"), ("v", "f32"))
     _check(lib().mapl_adamw_pack(values.array, packed.array, packed.count, _stream(stream)))
 
 

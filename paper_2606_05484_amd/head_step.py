@@ -19,7 +19,7 @@ else norm_fwd and norm_bwd.
 
 main() trains the head, the block and the projector (stiefel_step) on
 synthetic tokens whose activations carry their targets, and prints the loss
-and the time of every step.  The head and the block learn by plain SGD or by
+and the time of every step: its gradients and the update of the head and the block.  The head and the block learn by plain SGD or by
 AdamW on the gradient clipped to norm 1 (grad_norm, adamw_step), with states in
 fp32 (adamw) or in 8 bits (adamw8).
 """
@@ -117,6 +117,20 @@ class HeadStep:
             mapl.ckpt_encode_bwd(D, self.dZ[m], self.q[m], self.e[m], ids[m], U, A_s, B_s, self.dX[m], self.dU, 1, ws)
 
 
+class SGD:
+    """Plain steps of a dict of fp32 tensors by their gradients, under the same names; copies: bf16 copies to
+    keep up to date, by name."""
+
+    def __init__(self, params, grads, copies=(), lr=1.0):
+        self.params, self.grads, self.copies, self.lr = params, grads, dict(copies), lr
+
+    def step(self):
+        for name, p in self.params.items():
+            p.add_(self.grads[name], alpha=-self.lr)
+        for name, copy in self.copies.items():
+            copy.copy_(self.params[name])
+
+
 class AdamW:
     """The optimizer of a step's parameters: a dict of fp32 tensors and, under the same names, their
     gradients (fp32); copies: bf16 copies to keep up to date, by name.  What has one dimension does not decay."""
@@ -170,7 +184,10 @@ def main(argv=None):
         grads.update(step.block.grads)
     lr = a.lr if a.lr is not None else 1.0 if a.optimizer == "sgd" else 3e-3
     W = W32.to(bf)
-    adam = None if a.optimizer == "sgd" else AdamW(learned, grads, {"W": W}, lr, "8bit" if a.optimizer == "adamw8" else "f32")
+    if a.optimizer == "sgd":
+        optimizer = SGD(learned, grads, {"W": W}, lr)
+    else:
+        optimizer = AdamW(learned, grads, {"W": W}, lr, "8bit" if a.optimizer == "adamw8" else "f32")
     M = torch.zeros(1, d, r, device="cuda")
     wsU = mapl.workspace(mapl.workspace_bytes(None, mapl.CALL_STIEFEL, 1, d, r))
     spent = []
@@ -185,13 +202,8 @@ def main(argv=None):
         t0, t1 = (torch.cuda.Event(enable_timing=True) for _ in range(2))
         t0.record()
         step.gradients(X, ids, y, U, A, B, A, B, W, 1.0 / live, block=learned)
-        if adam:
-            adam.step()
+        optimizer.step()
         t1.record()
-        if not adam:
-            for name, p in learned.items():
-                p.add_(grads[name], alpha=-lr)
-            W = W32.to(bf)
         mapl.stiefel_step(1, d, r, U, step.dU, M, 0.02, 0.9, 5, 7, wsU)
         torch.cuda.synchronize()
         spent.append(t0.elapsed_time(t1))

@@ -403,13 +403,14 @@ def optim_params(g, p=None, m=None, v=None, e=None, p16=None, weight_decay=0.0, 
     """The tensors of an optimizer step: sequences of equal length (e, p16 and what a call does not
     use may be None); weight_decay and lr_scale are numbers or sequences of them."""
     count = len(g)
-    lists = {"g": g, "p": p, "m": m, "v": v, "e": e, "p16": p16}
+    lists = {name: None if x is None else tuple(x)  # (the caller's own lists may change)
+             for name, x in (("g", g), ("p", p), ("m", m), ("v", v), ("e", e), ("p16", p16))}
     each = lambda x: list(x) if hasattr(x, "__len__") else [x] * count
     decay, lr = each(weight_decay), each(lr_scale)
     for name, x in list(lists.items()) + [("weight_decay", decay), ("lr_scale", lr)]:
         if x is not None and len(x) != count:
             raise ValueError("%s has %d entries, g %d" % (name, len(x), count))
-    sizes = [t.numel() for t in g]
+    sizes = [t.numel() for t in lists["g"]]
     where, types = {}, {}
     for name, x in lists.items():
         if x is None:

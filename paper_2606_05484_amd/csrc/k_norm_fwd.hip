@@ -8,7 +8,8 @@
 //
 // Bound by HBM: 10 bytes a value where everything is bf16.  T = 32768, d = 2048 with a gated
 // branch whose two arrays are halves of one product's output 116 us, 5.8 TB/s (a large copy
-// here 4.9); T = 8192, d = 1024 14.1 us, 5.9 TB/s.  What carried it: one row a wave or a workgroup with all of
+// here 4.9); T = 8192, d = 1024 14.1 us, 5.9 TB/s; the residual add and
+// y alone (no norm of h, no gate) 101 us and 11.5, an fp32 stream with the gated bf16 block 163 and 26.6.  What carried it: one row a wave or a workgroup with all of
 // its loads first and no branch before them (143 us with one around each), rows by a scalar
 // base and 32-bit offsets, one-shot workgroups (with 2048 of them in a loop 150 and 129),
 // fp32 rows in runs of 1 KiB a wave and access, rows past 8192 on 512 lanes (T = 4096, d = 8256 with

@@ -24,7 +24,7 @@
 //
 // Bound by HBM: fp32 states 28 bytes a value (bf16 gradients and copy), 8 bits 16.03.  266 M
 // values: 1.30 ms, 5.7 TB/s, and 0.75 ms, 5.7 TB/s (a large copy here 4.9 TB/s); their states unpacked 0.45
-// ms, 5.9 TB/s.  All of a piece's loads first (four runs of four values a lane; two 1407 and 825 us, before
+// ms, 5.9 TB/s, packed 0.47, 5.6.  All of a piece's loads first (four runs of four values a lane; two 1407 and 825 us, before
 // the caches were passed by: 1390 and 799 with four), pieces of 4096 (of 2048 1421 and 801).
 #include "common.hpp"
 #include "kernels.hpp"

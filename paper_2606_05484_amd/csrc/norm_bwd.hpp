@@ -39,8 +39,13 @@ __global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormArgs g) {
   const float *w_post = or_ones(g.w_post), *scale = or_ones(g.scale), *w_pre = or_ones(g.w_pre);
   // Rows past 8192 values do not stay in registers: what a step needs is loaded again (from the
   // caches) a run of eight at a time.  d = 16384, T = 1024 in bf16: 106 us and 7 for the sum (held, with
-  // spills, 165 to 234).  Up to 12288 on 768 lanes, T = 4096, d = 8256 160 us, d = 12288 210 (on 512 lanes
-  // 172 and 212, 253 and 301 with room for 16384; past 12288 1024 lanes spill).
+  // more spills, 165 to 234).  Up to 12288 on 768 lanes, T = 4096, d = 8256 160 us, d = 12288 210 (on 512 lanes
+  // 172 and 212, 253 and 301 with room for 16384; past 12288 1024 lanes spill more).
+  // That spares most spills, not all, since the first pass's rows live beside the sums until both scales
+  // are known.  Registers spilled a lane: bf16 none up to 12288, past it 22 to 26 with branch and y; all fp32 16 or
+  // 17, past it 78 or 79; an fp32 stream with a bf16 block 39, past it 89; past 12288 without y up to 12 and 19; y
+  // alone none.  T = 4096 gated, d = 8256, 12288 and 16384: all fp32 281, 371, 759 us, an fp32 stream
+  // with a bf16 block 307, 376, 637, bf16 159, 209, 350.
   constexpr bool AGAIN = LANES * NV * 8 > 8192;
   float acc[NS][NV][8];
 #pragma unroll
